@@ -121,9 +121,10 @@ int stree_prepare(void);
  * (the problem statement of Sec. 3 "Formalization" fixes the operands; this call sizes
  * what the library needs beyond them).  Every intermediate of every kernel -- the tree
  * index, the decay-weighted mask, the state tile -- lives in LDS or registers, so the
- * answer is 0 for every valid `dims`, and no entry point takes a workspace argument.
- * Invalid `dims` (NULL, unknown dtype, a dimension outside the envelope) return
- * (size_t)-1.  conv_width and flags are not looked at.  Launches nothing.
+ * answer is 0 for every valid `dims`, and no entry point that takes them has a workspace argument.
+ * (The attention over a paged cache, further down, does take one, and has its own
+ * stree_attn_workspace_bytes.)  Invalid `dims` (NULL, unknown dtype, a dimension outside the
+ * envelope) return (size_t)-1.  conv_width and flags are not looked at.  Launches nothing.
  */
 size_t stree_workspace_bytes(const stree_dims *dims);
 
@@ -329,6 +330,179 @@ int stree_gate_norm(const stree_dims *dims, const void *y, const void *z, int64_
 int stree_linear_ssd(const stree_dims *dims, const void *x, const float *dt, const float *A,
                      const void *Bm, const void *Cm, const float *D, const void *h0, void *y,
                      void *h_out, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Attention layers of a hybrid model (the paper's end-to-end runs verify on one: half of its layers
+ * are attention).  The token tree that goes through the scan goes through these layers with the same
+ * parent array: a node sees the sequence's text and the nodes of its own path (the tree mask L).  Keys
+ * and values lie in a paged cache:
+ *   k      io [npages, nheads_kv, page, headdim]
+ *   v      io [npages, nheads_kv, headdim, page]    a page's tokens side by side: v is the transposed
+ *                                                   operand of the product with the probabilities
+ *   table  int32 [batch, max_pages]                 page numbers; token t of sequence b is row t % page
+ *                                                   of page table[b][t / page]
+ *   lengths int32 [batch]                           tokens that the cache holds of each sequence; a
+ *                                                   negative length is an idle row of the batch: nothing
+ *                                                   is read or written for it but zeros in its outputs
+ * Node i of sequence b stands in slot lengths[b] + i of the sequence (node order) until the commit, and
+ * at position lengths[b] + depth(i).  Query head h reads key/value head h / (nheads / nheads_kv).
+ * parent == NULL is the chain (a single new token, or a piece of a prompt): depth(i) = i, and nnodes may
+ * then be up to 2^24; with a tree nnodes <= STREE_MAX_NODES.
+ *
+ * Lengths, trees and page numbers are device data and are checked there, in this order; `seq_status[b]`
+ * (may be NULL) gets 0, or
+ *   STREE_SEQ_LENGTH  the nodes do not fit the table: lengths[b] + nnodes > max_pages * page
+ *   i + 1             first bad node of the tree
+ *   STREE_SEQ_ACCEPTED  accepted node outside [-1, nnodes)                              (stree_commit_kv)
+ *   STREE_SEQ_PAGE    a page that the call needs has a number outside [0, npages)
+ * and that sequence's outputs are zero-filled, its part of the cache left as it was.  No memory outside
+ * the arrays is touched whatever they hold.  Slots that no call has written are never used in a sum
+ * (they may hold NaN).
+ * ---------------------------------------------------------------------------------------------- */
+enum stree_seq_status {
+    STREE_SEQ_ACCEPTED = -1, /* accepted node outside [-1, nnodes) */
+    STREE_SEQ_LENGTH = -2,   /* a length does not fit the table (or the pool's counts contradict it) */
+    STREE_SEQ_PAGE = -3,     /* a page number is outside [0, npages), or the pool says that nobody holds the page */
+    STREE_SEQ_POOL = -4,     /* the pool has no pages left for this sequence */
+    STREE_SEQ_HELD = -5      /* fork: the target holds pages, or an earlier fork of the call has it */
+};
+
+/* The cache of one or more layers.  POD, host memory; the pointers in it are device memory. */
+typedef struct stree_kv {
+    int32_t nlayers;   /* layers behind k and v, one after the other; stree_tree_rope and stree_tree_attn take 1 */
+    int32_t npages;    /* pages of the pool, >= 1 */
+    int32_t page;      /* tokens a page: 16, 32, 64, 128 or 256 */
+    int32_t max_pages; /* entries of a row of `table`, >= 1; max_pages * page <= 2^30 */
+    int32_t nheads_kv; /* >= 1 */
+    int32_t headdim;   /* 1..256 */
+    int32_t io_dtype;  /* enum stree_dtype: the cache, queries, outputs */
+    int32_t reserved;  /* 0 */
+    void *k;           /* io [nlayers, npages, nheads_kv, page, headdim] */
+    void *v;           /* io [nlayers, npages, nheads_kv, headdim, page] */
+    int32_t *table;    /* int32 [batch, max_pages] */
+} stree_kv;
+
+enum stree_attn_flags {
+    STREE_ROPE_INTERLEAVED = 1, /* stree_tree_rope: pairs (2j, 2j+1); otherwise (j, j + rotary_dim/2) */
+    STREE_ATTN_PLAIN = 256      /* the plain kernels even where a tuned one applies (same results to rounding) */
+};
+
+/* Sizes of one attention layer's pass over the nodes.  POD, host memory. */
+typedef struct stree_attn {
+    int32_t batch;      /* 0 (a no-op) .. 65535 */
+    int32_t nnodes;     /* N >= 1; batch * nnodes * (nheads + 2 nheads_kv) < 2^31 */
+    int32_t nheads;     /* a multiple of kv->nheads_kv, <= 65535 */
+    int32_t flags;      /* enum stree_attn_flags */
+    int32_t rotary_dim; /* stree_tree_rope: rotated columns of a head, even, 0..headdim */
+    float eps;          /* stree_tree_rope: of the norms, >= 0 */
+    float rope_scale;   /* stree_tree_rope: factor of the rotated columns (1: none) */
+    float softmax_scale;/* stree_tree_attn: factor of <q, k>; 0 = 1 / sqrt(headdim) */
+    /* token strides in ELEMENTS (0 = dense); the batch stride is nnodes * token stride.  They let q | k | v
+     * be column ranges of one projection's output. */
+    int64_t q_stride_n, k_stride_n, v_stride_n;
+} stree_attn;
+
+enum stree_rope_scaling { STREE_ROPE_NONE = 0, STREE_ROPE_LINEAR = 1, STREE_ROPE_BASE = 2, STREE_ROPE_RAMP = 3 };
+
+/*
+ * Frequencies of the rotation, in turns a position: turns[j], j < rotary_dim/2, HOST memory (upload them
+ * once).  f_j = base^(-2j / rotary_dim) / (2 pi), stretched for contexts longer than those of the training:
+ *   NONE    f_j
+ *   LINEAR  f_j / factor
+ *   BASE    f_j with base * factor^(r / (r - 2)), r = rotary_dim (r > 2): the slowest pair turns `factor` times
+ *           slower, the fastest as before
+ *   RAMP    f_j (w + (1 - w) / factor), w = clamp((original * f_j - low) / (high - low), 0, 1): pairs that turn
+ *           fewer than `low` times within the original context are divided, those above `high` kept
+ * base > 0, factor >= 1, 0 <= low < high and original > 0 (RAMP), all finite; STREE_ERR_BAD_SHAPE otherwise.
+ * No GPU is used.
+ */
+int stree_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double low,
+                           double high, double original, double *turns);
+
+/*
+ * Queries, keys and values of the nodes made ready for stree_tree_attn, in one pass: RMS norm of each head of
+ * q and k, rotation to the node's position, k and v appended to the cache.
+ *   x^  = x / sqrt(mean over the head of x^2 + eps) * w         (q with q_norm, k with k_norm; NULL: x)
+ *   (u, w)_j -> rope_scale * (u cos a - w sin a, u sin a + w cos a),  a = 2 pi * position * turns[j]
+ *   q      io [B,N,H,P], k, v io [B,N,nheads_kv,P]   strides in `a`
+ *   q_norm, k_norm io [P] or NULL
+ *   turns  f64 [rotary_dim/2] (device); may be NULL with rotary_dim = 0
+ *   q_out  io [B,N,H,P] dense; MAY be q if that is dense.  Any other overlap with q, k or v: STREE_ERR_BAD_ALIAS
+ * The angle is reduced in 64 bits (exact to far positions), everything else is fp32 with one rounding of the
+ * result.  A sequence with a status: zeros in q_out, nothing appended.
+ */
+int stree_tree_rope(const stree_attn *a, const stree_kv *kv, const int32_t *parent, const int32_t *lengths,
+                    const void *q, const void *k, const void *v, const void *q_norm, const void *k_norm,
+                    const double *turns, void *q_out, int32_t *seq_status, void *hip_stream);
+
+/*
+ * Attention of the nodes over the cache and the nodes of their paths, whose rows stree_tree_rope appended:
+ *   out(b,i,h) = sum_t softmax_t(softmax_scale * <q(b,i,h), K(b,t)>) V(b,t),
+ *                t < lengths[b] or t = lengths[b] + j with j on the path of i
+ *   q   io [B,N,H,P] (q_stride_n)    out io [B,N,H,P] dense, must not overlap q
+ * One node is one new token's step.  Long sequences are split over workgroups, whose parts a second kernel
+ * joins: that takes device scratch of stree_attn_workspace_bytes(a, kv) bytes at `workspace`, aligned to 16
+ * bytes (NULL where that is 0; too few bytes: STREE_ERR_BAD_SHAPE), which holds nothing between calls; calls
+ * that may run at the same time need their own.  Sums, maxima and parts are fp32.  The tuned kernel rounds the
+ * probabilities to bf16 for the matrix units (their sum is that of the rounded ones).
+ * Infinities and NaN in the keys or values of a node reach the nodes that see it and no others.
+ * Tuned kernels: headdim a multiple of 8 (bf16) or 4 (fp32), 16-byte aligned q, k, v, out and a q stride of whole
+ * 16-byte pieces; a plain kernel takes the rest.
+ */
+int stree_tree_attn(const stree_attn *a, const stree_kv *kv, const int32_t *parent, const int32_t *lengths,
+                    const void *q, void *out, int32_t *seq_status, void *workspace, size_t workspace_bytes,
+                    void *hip_stream);
+
+/* Scratch of stree_tree_attn for these sizes ((size_t)-1: invalid sizes).  Pointers in `kv` and strides are not looked
+ * at.  Launches nothing. */
+size_t stree_attn_workspace_bytes(const stree_attn *a, const stree_kv *kv);
+
+/*
+ * Commit of the accepted node in the cache (what stree_commit_state is for the scan): the rows of its path, root
+ * first, move together behind the sequence's text, in every layer:
+ *   K, V [lengths[b] + t] = K, V [lengths[b] + p_t],  p_0 = root, .., p_d = accepted[b]
+ *   lengths_out[b] = lengths[b] + d + 1
+ * accepted[b] == -1, an idle sequence or one with a status: lengths_out[b] = lengths[b], nothing moves.
+ * parent NULL: a chain, whose rows stand where they should.  Of `a` only batch and nnodes are read.
+ *   lengths_out int32 [B]; MAY be lengths (STREE_ERR_BAD_ALIAS for any other overlap)
+ */
+int stree_commit_kv(const stree_attn *a, const stree_kv *kv, const int32_t *parent, const int32_t *accepted,
+                    const int32_t *lengths, int32_t *lengths_out, int32_t *seq_status, void *hip_stream);
+
+/* Who holds which page.  POD, host memory; device pointers, all of them read and written by the two calls below. */
+typedef struct stree_pool {
+    int32_t *held;  /* int32 [batch]: pages in each row of the table */
+    int32_t *refs;  /* int32 [npages]: rows that hold the page, 0 = free */
+    int32_t *free;  /* int32 [npages]: the first *nfree are the numbers of the free pages; taken from the end */
+    int32_t *nfree; /* int32 [1] */
+} stree_pool;
+
+/*
+ * Pages taken and given back: afterwards row b holds ceil(tokens[b] / page) pages (tokens[b] < 0: as many as before).
+ * First all rows that hold too many drop their last ones (the table's entries become -1); a page that no row holds any
+ * more becomes free, in the order of the entries (b, then j).  Then, in the order of b, the growing rows take free pages;
+ * a row for which there are not enough, and every growing row behind it, stays as it is with STREE_SEQ_POOL.
+ * tokens[b] beyond the table or held[b] outside [0, max_pages]: STREE_SEQ_LENGTH, row as it is.  A dropped entry whose
+ * number is bad or which nobody holds is dropped and frees nothing (STREE_SEQ_PAGE).  *nfree outside [0, npages]:
+ * STREE_SEQ_POOL for every row, nothing done.  batch <= 4096.  The outcome does not depend on timing.
+ * batch * max_pages <= 2^29.  k and v of `kv` may be NULL.  One call at a time may change a pool.
+ */
+int stree_resize_kv(const stree_kv *kv, const stree_pool *pool, int32_t batch, const int32_t *tokens,
+                    int32_t *seq_status, void *hip_stream);
+
+/*
+ * Sequences forked: for f < nforks sequence dst[f], which holds no pages, becomes a copy of src[f] (lengths, and as far
+ * as its text goes): full pages are shared, the page that src's last tokens stand in, if it is not full, is copied to a
+ * free page, whole, in every layer.  So no shared page is ever written to by appending.  The same src may be forked any
+ * number of times.  fork_status [nforks] (required) gets 0, or, with nothing done for that fork,
+ *   STREE_SEQ_LENGTH  src or dst outside [0, batch), src idle, or its length beyond the pages that it holds
+ *   STREE_SEQ_PAGE    a page of src has a bad number or is held by nobody
+ *   STREE_SEQ_HELD    dst holds pages (src == dst too, if it holds any), or an earlier fork that passes the checks above names it
+ *   STREE_SEQ_POOL    no page left (of those asked for in the order of f)
+ * Lengths and pages of src are those from before the call.  batch, nforks <= 4096.
+ */
+int stree_fork_kv(const stree_kv *kv, const stree_pool *pool, int32_t batch, int32_t nforks, const int32_t *src,
+                  const int32_t *dst, int32_t *lengths, int32_t *fork_status, void *hip_stream);
 
 #ifdef __cplusplus
 }

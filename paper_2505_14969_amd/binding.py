@@ -24,6 +24,10 @@ FLAG_CONV_SILU = 1
 FLAG_DT_SOFTPLUS = 2
 FLAG_FORCE_FMA = 256
 FLAG_GENERAL_MFMA = 1024
+ROPE_INTERLEAVED = 1
+ATTN_PLAIN = 256
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+SEQ_ACCEPTED, SEQ_LENGTH, SEQ_PAGE, SEQ_POOL, SEQ_HELD = -1, -2, -3, -4, -5
 MAX_NODES = 256
 
 
@@ -39,6 +43,21 @@ class StreeReplay(C.Structure):
                 ("x_stride_n", C.c_int64), ("b_stride_n", C.c_int64)]
 
 
+class StreeKv(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("nlayers", "npages", "page", "max_pages", "nheads_kv", "headdim", "io_dtype",
+                                         "reserved")] + [(n, C.c_void_p) for n in ("k", "v", "table")]
+
+
+class StreeAttn(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "nnodes", "nheads", "flags", "rotary_dim")] + \
+               [(n, C.c_float) for n in ("eps", "rope_scale", "softmax_scale")] + \
+               [(n, C.c_int64) for n in ("q_stride_n", "k_stride_n", "v_stride_n")]
+
+
+class StreePool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("held", "refs", "free", "nfree")]
+
+
 class StreeError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -50,7 +69,7 @@ _lib = None
 _host = None           # the native module, bound to the library's entry points
 _VP = C.c_void_p
 _ENTRIES = ("tree_conv", "tree_ssd", "commit_state", "tree_ssd_replay", "tree_conv_replay", "tree_step", "gate_norm",
-            "linear_ssd")
+            "linear_ssd", "tree_rope", "tree_attn", "attn_workspace_bytes", "commit_kv", "resize_kv", "fork_kv")
 
 
 def _bind(lib: C.CDLL) -> None:
@@ -100,6 +119,18 @@ def load() -> C.CDLL:
         lib.stree_gate_norm.restype = C.c_int
         for f in (lib.stree_tree_index, lib.stree_tree_conv, lib.stree_tree_ssd, lib.stree_commit_state,
                   lib.stree_tree_ssd_replay, lib.stree_tree_conv_replay, lib.stree_tree_step):
+            f.restype = C.c_int
+        kv, at, pool = C.POINTER(StreeKv), C.POINTER(StreeAttn), C.POINTER(StreePool)
+        lib.stree_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [_VP]
+        lib.stree_tree_rope.argtypes = [at, kv] + [_VP] * 11
+        lib.stree_tree_attn.argtypes = [at, kv] + [_VP] * 6 + [C.c_size_t, _VP]
+        lib.stree_attn_workspace_bytes.argtypes = [at, kv]
+        lib.stree_attn_workspace_bytes.restype = C.c_size_t
+        lib.stree_commit_kv.argtypes = [at, kv] + [_VP] * 6
+        lib.stree_resize_kv.argtypes = [kv, pool, C.c_int32] + [_VP] * 3
+        lib.stree_fork_kv.argtypes = [kv, pool, C.c_int32, C.c_int32] + [_VP] * 5
+        for f in (lib.stree_rope_frequencies, lib.stree_tree_rope, lib.stree_tree_attn, lib.stree_commit_kv,
+                  lib.stree_resize_kv, lib.stree_fork_kv):
             f.restype = C.c_int
         _lib, _host = lib, None            # (the native half is bound to this library at the first call that needs it)
     return _lib
@@ -239,3 +270,62 @@ def stree_linear_ssd(x, dt, A, Bm, Cm=None, D=None, h0=None, want_y: bool = True
     """Causal scan of T tokens per sequence: x [B,T,H,P], dt [B,T,H] f32, Bm/Cm [B,T,G,S].
     -> (y [B,T,H,P] or None, h_out [B,H,P,S] in the dtype of h0).  h_out may be h0 itself."""
     return _native().linear_ssd(x, dt, A, Bm, Cm, D, h0, want_y, out, h_out, dt_bias)
+
+
+
+# Attention layers of a hybrid model: the same trees over a paged cache.  One layer's cache is k_cache
+# [pages, heads, page, P] and v_cache [pages, heads, P, page]; commit and fork also take several layers' behind one
+# another ([layers, ...]).  table int32 [B, max_pages]; lengths int32 [B], negative for an idle row of the batch;
+# parent None is a chain.  `status` int32 [B] gets 0, a bad node + 1, or one of the SEQ_ codes.
+
+def stree_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                           low: float = 1.0, high: float = 4.0, original: float = 8192.0, device="cuda") -> torch.Tensor:
+    """Turns a position of each rotated pair, f64 [rotary_dim/2] on `device`; scaling "none", "linear", "base" or
+    "ramp" for contexts longer than `original`."""
+    turns = torch.empty(max(rotary_dim, 0) // 2, dtype=torch.float64)
+    _check(load().stree_rope_frequencies(rotary_dim, base, ROPE_SCALING[scaling], factor, low, high, original,
+                                         _ptr(turns) if turns.numel() else None), "stree_rope_frequencies")
+    return turns.to(device)
+
+
+def stree_tree_rope(parent, lengths, q, k, v, k_cache, v_cache, table, turns, q_norm=None, k_norm=None, eps: float = 1e-6,
+                    interleaved: bool = False, rope_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None):
+    """q [B,N,H,P], k, v [B,N,heads,P] (may be column views of one projection) -> rotated q [B,N,H,P]; rotated k
+    and v go into the cache's slots lengths[b] .. lengths[b] + N - 1.  q_norm, k_norm [P]: weights of an RMS norm of
+    each head in front of the rotation.  turns: stree_rope_frequencies().  out may be q itself where that is dense."""
+    return _native().tree_rope(parent, lengths, q, k, v, k_cache, v_cache, table, turns, q_norm, k_norm, eps, interleaved,
+                               rope_scale, out, status)
+
+
+def stree_tree_attn(parent, lengths, q, k_cache, v_cache, table, scale: Optional[float] = None,
+                    out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, plain: bool = False):
+    """q [B,N,H,P] -> attention of each node over the cache and its path, [B,N,H,P]; scale: 1/sqrt(P) unless given.
+    workspace: scratch of stree_attn_workspace() bytes; torch.empty's where none is given."""
+    return _native().tree_attn(parent, lengths, q, k_cache, v_cache, table, scale, out, status, workspace, plain)
+
+
+def stree_attn_workspace(q, k_cache, v_cache, table) -> int:
+    """Bytes of scratch that stree_tree_attn takes for these tensors' sizes."""
+    return _native().attn_workspace(q, k_cache, v_cache, table)
+
+
+def stree_commit_kv(parent, accepted, lengths, k_cache, v_cache, table, lengths_out: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None, nnodes: Optional[int] = None):
+    """Rows of the accepted path moved together, in every layer -> new lengths; lengths_out may be lengths itself.
+    A chain (parent None) says its nnodes."""
+    return _native().commit_kv(parent, accepted, lengths, k_cache, v_cache, table, lengths_out, status, nnodes)
+
+
+def stree_resize_kv(tokens, held, table, refs, free, nfree, page: int, status: Optional[torch.Tensor] = None):
+    """Rows of the table cut or grown to the pages of tokens[b] tokens (negative: as they are).  held [B], refs and
+    free [pages], nfree [1], all int32 and updated in place; returns held."""
+    return _native().resize_kv(tokens, held, table, refs, free, nfree, page, status)
+
+
+def stree_fork_kv(src, dst, lengths, held, table, refs, free, nfree, k_cache, v_cache,
+                  status: Optional[torch.Tensor] = None):
+    """Sequence dst[f] (which holds no pages) made a copy of src[f]: full pages shared, the partial one copied in every
+    layer; lengths, held, table and the pool are updated in place.  Returns the forks' status."""
+    return _native().fork_kv(src, dst, lengths, held, table, refs, free, nfree, k_cache, v_cache, status)

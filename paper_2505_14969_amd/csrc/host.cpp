@@ -31,6 +31,12 @@ struct Entry {
     decltype(&stree_tree_step) tree_step;
     decltype(&stree_gate_norm) gate_norm;
     decltype(&stree_linear_ssd) linear_ssd;
+    decltype(&stree_tree_rope) tree_rope;
+    decltype(&stree_tree_attn) tree_attn;
+    decltype(&stree_attn_workspace_bytes) attn_workspace_bytes;
+    decltype(&stree_commit_kv) commit_kv;
+    decltype(&stree_resize_kv) resize_kv;
+    decltype(&stree_fork_kv) fork_kv;
 };
 
 // A Python exception is set: leave the call.
@@ -508,6 +514,8 @@ PyObject *linear(const Args &a) {
     return pair(y, h);
 }
 
+#include "host_kv.hpp"
+
 template <PyObject *(*F)(const Args &), int kArgs>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -557,6 +565,7 @@ PyMethodDef methods[] = {
     STREE_METHOD("tree_step", step, 27),
     STREE_METHOD("gate_norm", gate, 6),
     STREE_METHOD("linear_ssd", linear, 11),
+    STREE_KV_METHODS(STREE_METHOD),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
