@@ -1,22 +1,12 @@
 // stree_tree_attn: attention of a tree's nodes over a paged cache and the nodes of their paths,
 //   out(b,i,h) = sum_t softmax_t(scale <q, K_t>) V_t,   t < length or t = length + j with j on the path of i,
-// one pass over the keys with the running maximum and sum of the softmax.
-#include "kv.hpp"
-#include "launch_kv.hpp"
+// one pass over the keys with the running maximum and sum of the softmax.  Here the plain kernel, for rows that are no whole
+// 16-byte pieces, and the choice; tree_attn_stream.hip has the tuned one.
+#include "attn.hpp"
 
 namespace stree {
 
 namespace {
-
-struct AttnArgs {
-    const int32_t *parent, *lengths;
-    const void *q;
-    void *out;
-    int32_t *status;
-    long q_sn;
-    int n, heads;
-    float scale;                       // of <q, k>, in units of log2(e): probabilities are powers of two
-};
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -116,11 +106,12 @@ hipError_t launch(const AttnArgs &a, const stree_kv &kv, int batch, hipStream_t 
 
 }  // namespace
 
-size_t tree_attn_workspace(const stree_attn &, const stree_kv &) { return 0; }
+size_t tree_attn_workspace(const stree_attn &a, const stree_kv &kv) { return attn_stream_workspace(a, kv); }
 
 hipError_t launch_tree_attn(const stree_attn &a, const stree_kv &kv, const int32_t *parent, const int32_t *lengths, const void *q,
-                            void *out, int32_t *status, void *, hipStream_t st) {
+                            void *out, int32_t *status, void *workspace, hipStream_t st) {
     const AttnArgs r = {parent, lengths, q, out, status, (long)a.q_stride_n, a.nnodes, a.nheads, a.softmax_scale * 1.44269504088896340736f};
+    if (!(a.flags & STREE_ATTN_PLAIN) && attn_stream_supported(a, kv, q, out)) return launch_attn_stream(a, kv, r, workspace, st);
     return kv.io_dtype == STREE_BF16 ? launch<bf16_t>(r, kv, a.batch, st) : launch<float>(r, kv, a.batch, st);
 }
 
