@@ -15,20 +15,152 @@ struct AttnArgs {
     float scale;                       // of <q, k>, in units of log2(e): probabilities are powers of two
 };
 
-constexpr int kPieceKeys = 256;        // keys of a piece, at least: 64 for each wave
-constexpr int kWorkgroups = 768;       // workgroups that a call is split into, if its keys allow: three to a CU
+constexpr int kTileKeys = 128;         // keys that the work is counted in: a step of bf16 keys for each of four waves
 
-// The host knows how far the table reaches, the device how long the sequences are: the grid has `pieces` workgroups for each
-// (sequence, head, tile of rows), and a sequence uses as many of them as its keys fill.
+// The work of a call is B sequences x heads x tiles of their keys, which the device alone knows how many there are of: every
+// worker (a workgroup, or one for each tile of rows) takes an equal share of the tiles in that order, so that lengths may
+// differ as they like, and a sequence's head is cut where a share ends.  Parts of a head that was cut go to scratch, slot
+// (worker + unit): going on to the next part raises one of the two, or both.
 struct AttnSplit {
-    int pieces, tiles, rows, units;    // rows: kept of each tile (fewer than the tile's where there is only one)
+    int workers, tiles, rows, batch;   // tiles of rows; rows: kept of each (fewer than the tile's where there is only one)
     Divisor group;                     // query heads of a key/value head
-    float *parts;                      // [units, tiles, rows, dim]: sums of 2^(s - top) V
-    float2 *sums;                      // [units, tiles, rows]: (top, sum of 2^(s - top)); a negative sum: -attn_code()
+    int2 *plan;                        // [units]: first worker of the unit and how many, written by the first
+    float2 *sums;                      // [workers + units, tiles, rows]: (top, sum of 2^(s - top)); a negative sum: -attn_code()
+    float *parts;                      // [workers + units, tiles, rows, dim]: sums of 2^(s - top) V
     explicit AttnSplit(int r) : group(r) {}
-    __device__ __forceinline__ int piece_keys(int keys) const {
-        const int each = (keys + pieces - 1) / pieces;
-        return max((each + 127) & ~127, kPieceKeys);
+};
+
+// A value that all lanes of a wave have alike, for the compiler to keep it once.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// The same value, which the compiler takes for another: what is worked out from it inside a loop is not moved in front of the
+// loop, to lie in registers all the while.
+__device__ __forceinline__ int again(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+__device__ __forceinline__ int64_t quotient64(int64_t a, int64_t d) {       // a >= 0, d > 0; most are small
+    return (a | d) >> 31 ? a / d : (int64_t)((uint32_t)a / (uint32_t)d);
+}
+
+// Equal shares of `total` tiles: the first `more` workers take one more than `each`.
+struct Shares {
+    int64_t each, bound;
+    int workers, more;
+    __device__ __forceinline__ Shares(int64_t total, int most) {
+        workers = total < most ? (int)total : most;
+        each = uniform(quotient64(total, workers));
+        more = uniform((int)(total - each * workers));
+        bound = (each + 1) * more;
+    }
+    __device__ __forceinline__ int64_t begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int worker(int64_t x) const {
+        return (int)(x < bound ? quotient64(x, each + 1) : more + quotient64(x - bound, each));
+    }
+};
+
+// Tiles of a sequence; one for a sequence that gets zeros.
+template <typename T>
+__device__ __forceinline__ int tiles_of(const KvView<T> &kv, int len, int n) {
+    return len < 0 || !kv.fits((int64_t)len + n) ? 1 : (len + n + kTileKeys - 1) / kTileKeys;
+}
+
+// Where a worker stands: head g of sequence b, of whose `tiles` tiles it takes [t0, t1); `left` tiles of its share from t0 on.
+struct Share {
+    int b, g, t0, t1, tiles, len;
+    int64_t left;
+    int workers;                       // of this call: none without a tile
+    int64_t x;
+    Shares shares;
+
+    // Finds the worker's first tile; the whole workgroup calls it (`first`: kThreads numbers of LDS, free again behind the next
+    // barrier).  Up to 64 sequences each wave finds it by itself.
+    template <typename T>
+    __device__ __forceinline__ static Share start(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, int worker, int64_t *first) {
+        const int lane = threadIdx.x & 63;
+        if (sp.batch <= 64) {
+            const int l = lane < sp.batch ? a.lengths[lane] : 0, mine = lane < sp.batch ? tiles_of(kv, l, a.n) : 0;
+            int sum = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int u = __shfl_up(sum, o);
+                if (lane >= o) sum += u;
+            }
+            Share s(Shares((int64_t)__builtin_amdgcn_readlane(sum, 63) * kv.heads, sp.workers));
+            if (worker >= s.workers) return s;
+            s.x = s.shares.begin(worker);
+            s.b = uniform(__ffsll((long long)__ballot((int64_t)sum * kv.heads > s.x)) - 1);
+            s.tiles = __builtin_amdgcn_readlane(mine, s.b), s.len = __builtin_amdgcn_readlane(l, s.b);
+            s.place(s.x - (int64_t)(__builtin_amdgcn_readlane(sum, s.b) - s.tiles) * kv.heads, worker);
+            return s;
+        }
+        // tiles in front of every run of sequences, one run a thread
+        const int run = (sp.batch + kThreads - 1) / kThreads, wave = threadIdx.x >> 6;
+        int64_t sum = 0;
+        for (int y = threadIdx.x * run; y < min((int)(threadIdx.x + 1) * run, sp.batch); ++y) sum += tiles_of(kv, a.lengths[y], a.n);
+        const int64_t mine = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t u = __shfl_up(sum, o);
+            if (lane >= o) sum += u;
+        }
+        if (lane == 63) first[wave] = sum;
+        __syncthreads();
+        int64_t total = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) {
+            const int64_t u = first[w];
+            if (w < wave) sum += u;
+            total += u;
+        }
+        __syncthreads();
+        first[threadIdx.x] = sum - mine;
+        __syncthreads();
+        Share s(Shares(uniform(total) * kv.heads, sp.workers));
+        if (worker >= s.workers) return s;
+        s.x = s.shares.begin(worker);
+        int lo = 0, hi = kThreads;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] * kv.heads <= s.x) lo = mid;
+            else hi = mid;
+        }
+        lo = uniform(lo);
+        int64_t at = uniform(first[lo]) * kv.heads;
+        for (s.b = min(lo * run, sp.batch - 1);; ++s.b) {
+            s.len = a.lengths[s.b], s.tiles = tiles_of(kv, s.len, a.n);
+            if (s.x < at + (int64_t)s.tiles * kv.heads || s.b == sp.batch - 1) break;
+            at += (int64_t)s.tiles * kv.heads;
+        }
+        s.place(s.x - at, worker);
+        return s;
+    }
+    __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
+    // on to the next head or sequence; false at the end of the share
+    template <typename T>
+    __device__ __forceinline__ bool next(const AttnArgs &a, const KvView<T> &kv) {
+        const int done = t1 - t0;
+        x += done, left -= done;
+        if (left <= 0) return false;
+        t0 = 0;
+        if (++g == kv.heads) {
+            g = 0, ++b;
+            len = a.lengths[b], tiles = tiles_of(kv, len, a.n);
+        }
+        t1 = (int)min((int64_t)tiles, left);
+        return true;
+    }
+
+  private:
+    __device__ __forceinline__ explicit Share(const Shares &s) : left(0), workers(s.workers), shares(s) {}
+    __device__ __forceinline__ void place(int64_t within, int worker) {
+        g = uniform((int)quotient64(within, tiles)), t0 = uniform((int)(within - (int64_t)g * tiles));
+        left = shares.begin(worker + 1) - x;
+        t1 = (int)min((int64_t)tiles, t0 + left);
     }
 };
 

@@ -1,7 +1,7 @@
 // The tuned kernel of stree_tree_attn: the cache streamed once from memory straight into operand registers.
 //
-// A workgroup takes 16, 32 or 64 query rows (node, head) of one key/value head and one piece of the sequence's keys; each of
-// its four waves walks a quarter of the piece by itself, STEP keys at a time.  Products are formed transposed, so that in
+// A workgroup takes 16, 32 or 64 query rows (node, head) of one key/value head and one piece of the sequence's keys; its
+// four waves take the piece's keys in turn, STEP at a time.  Products are formed transposed, so that in
 // every accumulator a lane owns one query row (column lane % 16):
 //   S^T = K Q^T,   P = 2^(S - m),   O^T += V^T P^T
 // Which key stands in which row of S^T is free, so keys are read in the order that makes a lane's probabilities the very
@@ -18,6 +18,7 @@ namespace {
 
 constexpr float kSlack = 8.f;
 constexpr int kWaves = kThreads / 64;
+constexpr int kChip = 256;                            // CUs
 
 // 16 bytes of a row as a matrix operand, and the two products, per type.
 template <typename T>
@@ -113,59 +114,81 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     typedef StreamShape<T, PP, MB> Shape;
     constexpr int E = M::E, KB = M::KB, STEP = 16 * KB, NK = PP / (4 * E), NP = PP / 16, ROWS = Shape::kRows, SL = Shape::kSlice, LD = Shape::kLd;
     struct Index { TreeLds tree; uint32_t bits[kMaxNodes * kMaxWords]; };
-    __shared__ union { Index index; float o[kWaves][ROWS][LD]; } lds;
+    __shared__ union { Index index; float o[kWaves][ROWS][LD]; int64_t first[kThreads + 1]; } lds;
     __shared__ float ml[kWaves][ROWS][2];
-    // The workgroups of one piece's row tiles follow one another on one XCD, whose L2 they share the piece through.
-    const int tile = (int)(blockIdx.x >> 3) % sp.tiles, unit = ((int)(blockIdx.x >> 3) / sp.tiles) * 8 + (int)(blockIdx.x & 7);
-    if (unit >= sp.units) return;
-    const int piece = unit % sp.pieces, g = unit / sp.pieces % kv.heads, b = unit / sp.pieces / kv.heads;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4, P = kv.dim;
-    const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS;
-    const int len = a.lengths[b];
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), P = kv.dim;
+    // The row tiles of one worker follow one another on one XCD, whose L2 they share the keys and values through.
+    const int tile = (int)(blockIdx.x >> 3) % sp.tiles, worker = ((int)(blockIdx.x >> 3) / sp.tiles) * 8 + (int)(blockIdx.x & 7);
+    if (worker >= sp.workers) return;
+    const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, mine = min(ROWS, rows - row0);
     T *const out = static_cast<T *>(a.out);
-    // pieces of this sequence; what this workgroup's rows see of its piece
-    int bad = 0, count = 1;
-    int k0 = 0, k1 = 0, whole = 0;
-    if (len >= 0) {
-        if (!kv.fits((int64_t)len + a.n)) {
-            bad = STREE_SEQ_LENGTH;
-        } else {
-            const int keys = len + a.n, each = sp.piece_keys(keys);
-            count = (keys + each - 1) / each;
-            if (piece < count) {
-                const int last = sp.group.quotient(min(row0 + ROWS, rows) - 1);
-                k0 = piece * each, whole = min(k0 + each, keys);
-                k1 = min(whole, len + last + 1);
-                if (whole > len && a.parent) bad = index_nodes(lds.index.tree, lds.index.bits, a.parent, b, a.n, (a.n + 31) / 32);
-            }
-        }
-    }
-    if (piece >= count) return;
+    Share at = Share::start(a, kv, sp, worker, lds.first);
+    if (worker >= at.workers) return;
 
-    float m[MB], base[MB], l[MB];
-    floatx4 o[MB][NP];
+    // What the waves are at: the piece's keys up to k1 (these rows see no more of it) and `whole` (where it ends), the page
+    // numbers, the queries, and the keys and values of the next step, always on their way.  The waves take the piece's steps
+    // in turn: a line of a page of many tokens holds the values of several steps, which are then asked for at nearly the same
+    // time.
+    const int shift = kv.shift, mask = kv.mask();
+    const size_t block = (size_t)P << shift;
+    const bool lines = (sizeof(T) << shift) <= 64;
+    int k0 = 0, k1 = 0, whole = 0, end = 0;
+    PageWalk<T> walk;
+    Frag q[MB][NK], kf[KB][NK], vf[NP];
+    const T *kp, *vp;                                  // this lane's key row and first value of the step
+    // Keys in the order that gives lane group `grp` the tokens E grp .. E grp + E - 1 of the step.
+    auto place = [&](int t, int col, int grp) {
+        const int ktok = E * (col >> 2) + (col & 3), vtok = E * grp, vrow = WHOLE || col < P ? col : 0;
+        walk.reach(kv, at.b, t >> shift, end, lane);
+        const int pa = walk.at(t >> shift);
+        int pk = pa, pv = pa;
+        if (STEP > 16 && shift == 4) {                 // a step of two pages
+            const int pb = (t >> 4) + 1 < end ? walk.at((t >> 4) + 1) : pa;
+            pk = ktok < 16 ? pa : pb, pv = vtok < 16 ? pa : pb;
+        }
+        kp = kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + ktok) & mask) * P + grp * E;
+        vp = kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)vrow << shift) + ((t + vtok) & mask);
+    };
+    auto load_k = [&](int grp) {
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        m[mb] = -INFINITY, base[mb] = 0.f, l[mb] = 0.f;
+        for (int x = 0; x < KB; ++x)
 #pragma unroll
-        for (int p = 0; p < NP; ++p) o[mb][p] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    const int part = ((k1 - k0 + kWaves - 1) / kWaves + STEP - 1) / STEP * STEP;
-    const int w0 = k0 + wave * part, w1 = min(w0 + part, k1);
-    bool missing = false;
-    if (bad == 0 && w0 < w1) {
-        const int shift = kv.shift, mask = kv.mask(), end = ((w1 - 1) >> shift) + 1;
-        PageWalk<T> walk;
-        walk.start(kv, b, w0 >> shift, end, lane);
+            for (int c = 0; c < NK; ++c)
+                kf[x][c] = __builtin_bit_cast(Frag, *reinterpret_cast<const uint4 *>(kp + 4 * x * P + (WHOLE || (4 * c + grp) * E < P ? 4 * c * E : -grp * E)));
+    };
+    // Values of a page of up to 64 bytes a row come in whole lines, once: with the streaming hint.  Larger pages have the values
+    // of several steps in a line, and a line of keys is asked for twice: without it.
+    auto load_v = [&](int col) {
+        auto from = [&](int p) { return reinterpret_cast<const uint4 *>(vp + (WHOLE || 16 * p + col < P ? (size_t)(16 * p) << shift : (size_t)0)); };
+        if (lines) {
+            asm volatile("; whole lines");             // (the two kinds of loads are not to be made one)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) vf[p] = __builtin_bit_cast(Frag, load_stream16(from(p)));
+            asm volatile("; whole lines");
+        } else {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) vf[p] = __builtin_bit_cast(Frag, *from(p));
+        }
+    };
+    // A new piece: everything that does not wait for its first keys.
+    auto enter = [&]() {
+        const int col = again(lane) & 15, grp = again(lane) >> 4;
+        k0 = k1 = whole = 0;
+        if (at.len >= 0 && kv.fits((int64_t)at.len + a.n)) {
+            const int last = sp.group.quotient(min(row0 + ROWS, rows) - 1);
+            k0 = at.t0 * kTileKeys, whole = min(at.t1 * kTileKeys, at.len + a.n);
+            k1 = min(whole, at.len + last + 1);
+        }
+        walk.bad = false;
+        const int t = k0 + wave * STEP;
+        if (t >= k1) return;
+        end = ((k1 - 1) >> shift) + 1;
+        walk.start(kv, at.b, t >> shift, end, lane);
         // queries: row `col` of each block, 16 bytes at column (4 c + grp) E; zeros behind the head and the last row
-        Frag q[MB][NK];
-        int node[MB];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            const int r = row0 + mb * 16 + col, rr = min(r, rows - 1);
-            const int i = sp.group.quotient(rr), h = g * R + rr - i * R;
-            node[mb] = i;
-            const T *src = static_cast<const T *>(a.q) + ((size_t)b * a.n + i) * a.q_sn + (size_t)h * P;
+            const int r = row0 + mb * 16 + col, rr = min(r, rows - 1), i = sp.group.quotient(rr), h = at.g * R + rr - i * R;
+            const T *src = static_cast<const T *>(a.q) + ((size_t)at.b * a.n + i) * a.q_sn + (size_t)h * P;
 #pragma unroll
             for (int c = 0; c < NK; ++c) {
                 const int x = (4 * c + grp) * E;
@@ -174,36 +197,32 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 q[mb][c] = __builtin_bit_cast(Frag, there ? v : make_uint4(0u, 0u, 0u, 0u));
             }
         }
-        // Places within a page: keys in the order that gives lane group `grp` the tokens E grp .. E grp + E - 1 of the step.
-        const int ktok = E * (col >> 2) + (col & 3), vtok = E * grp, vrow = WHOLE || col < P ? col : 0;
-        const size_t block = (size_t)P << shift;
-        const T *kp, *vp;                              // this lane's key row and first value of the step
-        auto place = [&](int t) {
-            walk.reach(kv, b, t >> shift, end, lane);
-            const int pa = walk.at(t >> shift);
-            int pk = pa, pv = pa;
-            if (STEP > 16 && shift == 4) {             // a step of two pages
-                const int pb = (t >> 4) + 1 < end ? walk.at((t >> 4) + 1) : pa;
-                pk = ktok < 16 ? pa : pb, pv = vtok < 16 ? pa : pb;
-            }
-            kp = kv.k + ((size_t)pk * kv.heads + g) * block + (size_t)((t + ktok) & mask) * P + grp * E;
-            vp = kv.v + ((size_t)pv * kv.heads + g) * block + ((size_t)vrow << shift) + ((t + vtok) & mask);
-        };
-        Frag kf[KB][NK], vf[NP];
-        auto load_k = [&]() {
+        place(t, col, grp);
+        load_k(grp);
+        load_v(col);
+    };
+    enter();
+    for (;;) {
+        // tiles [t0, t1) of head g of sequence b
+        const int b = at.b, g = at.g, len = at.len, w1 = k1, col = again(lane) & 15, grp = again(lane) >> 4, vtok = E * grp;
+        const int unit = b * kv.heads + g;
+        const bool direct = at.whole();
+        if (at.t0 == 0 && sp.plan && tile == 0 && threadIdx.x == 0)
+            sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
+        int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
+        if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_nodes(lds.index.tree, lds.index.bits, a.parent, b, a.n, (a.n + 31) / 32);
+
+        float m[MB], base[MB], l[MB];
+        floatx4 o[MB][NP];
+        int node[MB];
 #pragma unroll
-            for (int x = 0; x < KB; ++x)
+        for (int mb = 0; mb < MB; ++mb) {
+            node[mb] = sp.group.quotient(min(row0 + mb * 16 + col, rows - 1));
+            m[mb] = -INFINITY, base[mb] = 0.f, l[mb] = 0.f;
 #pragma unroll
-                for (int c = 0; c < NK; ++c) kf[x][c] = __builtin_bit_cast(Frag, load_stream16(kp + 4 * x * P + (WHOLE || (4 * c + grp) * E < P ? 4 * c * E : -grp * E)));
-        };
-        auto load_v = [&]() {
-#pragma unroll
-            for (int p = 0; p < NP; ++p) vf[p] = __builtin_bit_cast(Frag, load_stream16(vp + (WHOLE || 16 * p + col < P ? (size_t)(16 * p) << shift : (size_t)0)));
-        };
-        place(w0);
-        load_k();
-        load_v();
-        for (int t = w0; t < w1; t += STEP) {
+            for (int p = 0; p < NP; ++p) o[mb][p] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        for (int t = k0 + wave * STEP; t < w1; t += kWaves * STEP) {
             floatx4 s[MB][KB];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
@@ -214,10 +233,10 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                     for (int c = 0; c < NK; ++c) s[mb][x] = M::qk(kf[x][c], q[mb][c], s[mb][x]);
                 }
             __builtin_amdgcn_sched_barrier(0);         // (the next keys take these keys' registers, not others)
-            const bool more = t + STEP < w1;
+            const bool more = t + kWaves * STEP < w1;
             if (more) {
-                place(t + STEP);
-                load_k();
+                place(t + kWaves * STEP, col, grp);
+                load_k(grp);
             }
             const bool tail = t + STEP > len || t + STEP > w1;
             uint32_t seen[MB];
@@ -228,7 +247,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 top[mb] = -INFINITY;
                 if (tail) {
                     seen[mb] = seen_nodes<E>(lds.index.bits, (a.n + 31) / 32, a.parent != nullptr, node[mb], t + vtok - len);
-                    const int left = w1 - t - vtok;            // (keys behind the wave's last)
+                    const int left = w1 - t - vtok;            // (keys behind the last)
                     seen[mb] &= left >= E ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
                 }
 #pragma unroll
@@ -306,160 +325,225 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (more) load_v();
+            if (more) load_v(col);
         }
-        missing = walk.bad;
-    }
-    // (pages of the piece that only later rows see)
-    if (bad == 0)
-        for (int j = (k1 >> kv.shift) + (int)threadIdx.x; j < (whole + kv.mask()) >> kv.shift; j += kThreads)
-            missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
-    if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
+        // (pages of the piece that only later rows see)
+        int missing = walk.bad;
+        for (int j = (k1 >> shift) + (int)threadIdx.x; j < (whole + mask) >> shift; j += kThreads) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
+        if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
+        // the next piece's first keys are on their way while this one's waves are joined
+        const bool more = at.next(a, kv);
+        if (more) enter();
 
-    // join the waves
+        // join the waves
+        {
+        const int tid = again((int)threadIdx.x), col = tid & 15, grp = (tid >> 4) & 3;
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        l[mb] += __shfl_xor(l[mb], 16);
-        l[mb] += __shfl_xor(l[mb], 32);
-        if (grp == 0) ml[wave][mb * 16 + col][0] = m[mb], ml[wave][mb * 16 + col][1] = l[mb];
-    }
-    __syncthreads();
-    float keep[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        const int r = mb * 16 + col;
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][r][0]);
-        // (rows without a finite score: their sums stay what they are)
-        keep[mb] = m[mb] == top ? 1.f : m[mb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mb] - top);
-    }
-    const int mine = min(ROWS, rows - row0);
-    const bool dead = len < 0 || bad != 0, direct = count == 1;
-    const size_t slot = ((size_t)unit * sp.tiles + tile) * sp.rows;
-    for (int c0 = 0; c0 < PP; c0 += SL) {
-        if (c0) __syncthreads();
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int x = 0; x < NP; ++x)
-                if (16 * x >= c0 && 16 * x < c0 + SL)
-                    *reinterpret_cast<floatx4 *>(&lds.o[wave][mb * 16 + col][16 * x - c0 + 4 * grp]) = o[mb][x] * keep[mb];
+        for (int mb = 0; mb < MB; ++mb) {
+            l[mb] += __shfl_xor(l[mb], 16);
+            l[mb] += __shfl_xor(l[mb], 32);
+            if (grp == 0) ml[wave][mb * 16 + col][0] = m[mb], ml[wave][mb * 16 + col][1] = l[mb];
+        }
         __syncthreads();
-        for (int x = threadIdx.x; x < mine * (SL / 4); x += kThreads) {
-            const int r = x / (SL / 4), c = c0 + x % (SL / 4) * 4;
-            if (c >= P) continue;
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-            float top = -INFINITY, sum = 0.f;
+        float keep[MB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const int r = mb * 16 + col;
+            float top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][r][0]);
+            // (rows without a finite score: their sums stay what they are)
+            keep[mb] = m[mb] == top ? 1.f : m[mb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mb] - top);
+        }
+        const bool dead = len < 0 || bad != 0;
+        const size_t slot = ((size_t)(worker + unit) * sp.tiles + tile) * sp.rows;
+        for (int c0 = 0; c0 < PP; c0 += SL) {
+            if (c0) __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float mw = ml[w][r][0], f = mw == top ? 1.f : mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                sum += ml[w][r][1] * f;
-                v += *reinterpret_cast<const floatx4 *>(&lds.o[w][r][c - c0]);
-            }
-            if (direct) {
-                const int i = sp.group.quotient(row0 + r), h = g * R + row0 + r - i * R;
-                T *dst = out + (((size_t)b * a.n + i) * a.heads + h) * P + c;
+            for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) from_f32(dead ? 0.f : v[e] / sum, dst[e]);
-            } else {
-                if (!dead) *reinterpret_cast<floatx4 *>(sp.parts + (slot + r) * P + c) = v;
-                if (c == 0) sp.sums[slot + r] = make_float2(top, bad ? -(float)attn_code(bad) : sum);
+                for (int x = 0; x < NP; ++x)
+                    if (16 * x >= c0 && 16 * x < c0 + SL)
+                        *reinterpret_cast<floatx4 *>(&lds.o[wave][mb * 16 + col][16 * x - c0 + 4 * grp]) = o[mb][x] * keep[mb];
+            __syncthreads();
+            for (int y = tid; y < mine * (SL / 4); y += kThreads) {
+                const int r = y / (SL / 4), c = c0 + y % (SL / 4) * 4;
+                if (c >= P) continue;
+                floatx4 v = {0.f, 0.f, 0.f, 0.f};
+                float top = -INFINITY, all = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][r][0]);
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float mw = ml[w][r][0], f = mw == top ? 1.f : mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
+                    all += ml[w][r][1] * f;
+                    v += *reinterpret_cast<const floatx4 *>(&lds.o[w][r][c - c0]);
+                }
+                if (direct) {
+                    const int i = sp.group.quotient(row0 + r), h = g * R + row0 + r - i * R;
+                    T *dst = out + (((size_t)b * a.n + i) * a.heads + h) * P + c;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) from_f32(dead ? 0.f : v[e] / all, dst[e]);
+                } else {
+                    if (!dead) *reinterpret_cast<floatx4 *>(sp.parts + (slot + r) * P + c) = v;
+                    if (c == 0) sp.sums[slot + r] = make_float2(top, bad ? -(float)attn_code(bad) : all);
+                }
             }
         }
+        }
+        if (direct && a.status && g == 0 && tile == 0 && threadIdx.x == 0) a.status[b] = bad;
+        if (!more) break;
+        __syncthreads();                                   // (LDS is read)
     }
-    if (direct && a.status && g == 0 && tile == 0 && threadIdx.x == 0) a.status[b] = bad;
 }
 
-// Joins the pieces of a row: a workgroup per row, lanes over columns and pieces.
+// Joins the parts of the rows of a unit that was cut: workgroup (some rows, unit).  A few parts: a row's columns over lanes,
+// as many rows at once as there are lanes for.  Many: one row at a time, lanes over columns and parts.
+constexpr int kFewParts = 8;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<T> kv, AttnSplit sp, int tile_rows) {
     __shared__ float4 acc[kThreads];
-    __shared__ float2 ms[kThreads];
-    const int g = blockIdx.y % kv.heads, b = blockIdx.y / kv.heads, P = kv.dim, R = sp.group.d, tid = threadIdx.x;
-    const int len = a.lengths[b];
-    if (len < 0 || !kv.fits((int64_t)len + a.n)) return;
-    const int keys = len + a.n, each = sp.piece_keys(keys), count = (keys + each - 1) / each;
-    if (count == 1) return;
-    const int row = blockIdx.x, tile = row / tile_rows, r = row - tile * tile_rows;
-    const size_t unit0 = ((size_t)b * kv.heads + g) * sp.pieces;
-    auto slot = [&](int s) { return ((unit0 + s) * sp.tiles + tile) * sp.rows + r; };
-    // maximum and sum of all pieces, or what one of them found wrong (a negative sum)
-    float top = -INFINITY;
-    int code = INT32_MAX;
-    for (int s = tid; s < count; s += kThreads) {
-        const float2 v = sp.sums[slot(s)];
-        top = fmaxf(top, v.x);
-        if (v.y < 0.f) code = min(code, (int)-v.y);
+    __shared__ float factor[kThreads], red[kWaves][2];
+    const int unit = blockIdx.y, P = kv.dim, R = sp.group.d, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int2 plan = sp.plan[unit];
+    if (plan.y == 1) return;
+    const int g = unit % kv.heads, b = unit / kv.heads, rows = a.n * R;
+    const int quads = P / 4, over = kThreads / quads, c = tid % quads, s0 = tid / quads;
+    const size_t step = (size_t)sp.tiles * sp.rows;
+    if (plan.y <= kFewParts) {
+        if (s0 >= over) return;
+        for (int row = blockIdx.x * over + s0; row < rows; row += gridDim.x * over) {
+            const int tile = row / tile_rows, r = row - tile * tile_rows;
+            const size_t slot0 = ((size_t)(plan.x + unit) * sp.tiles + tile) * sp.rows + r;
+            float2 w[kFewParts];
+            float4 p[kFewParts];
+            float top = -INFINITY, code = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < kFewParts; ++s) {
+                w[s] = make_float2(-INFINITY, 0.f);
+                if (s < plan.y) {
+                    w[s] = sp.sums[slot0 + s * step];
+                    p[s] = *reinterpret_cast<const float4 *>(sp.parts + (slot0 + s * step) * P + 4 * c);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < kFewParts; ++s) {
+                top = fmaxf(top, w[s].x);
+                if (w[s].y < 0.f) code = fmaxf(code, w[s].y);
+            }
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            float sum = 0.f;
+#pragma unroll
+            for (int s = 0; s < kFewParts; ++s)
+                if (s < plan.y) {
+                    const float f = w[s].x == top ? 1.f : w[s].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w[s].x - top);
+                    sum += w[s].y * f;
+                    v.x = fmaf(p[s].x, f, v.x), v.y = fmaf(p[s].y, f, v.y), v.z = fmaf(p[s].z, f, v.z), v.w = fmaf(p[s].w, f, v.w);
+                }
+            if (code > -INFINITY) v = make_float4(0.f, 0.f, 0.f, 0.f), sum = 1.f;
+            const int i = sp.group.quotient(row), h = g * R + row - i * R;
+            T *const dst = static_cast<T *>(a.out) + (((size_t)b * a.n + i) * a.heads + h) * P + 4 * c;
+            from_f32(v.x / sum, dst[0]), from_f32(v.y / sum, dst[1]), from_f32(v.z / sum, dst[2]), from_f32(v.w / sum, dst[3]);
+            if (a.status && g == 0 && row == 0 && c == 0) a.status[b] = code > -INFINITY ? attn_status((int)-code) : 0;
+        }
+        return;
     }
-    ms[tid] = make_float2(top, __int_as_float(code));
-    __syncthreads();
-    for (int o = kThreads / 2; o > 0; o >>= 1) {
-        if (tid < o) {
-            const float2 u = ms[tid], v = ms[tid + o];
-            ms[tid] = make_float2(fmaxf(u.x, v.x), __int_as_float(min(__float_as_int(u.y), __float_as_int(v.y))));
+    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int tile = row / tile_rows, r = row - tile * tile_rows;
+        const size_t slot0 = ((size_t)(plan.x + unit) * sp.tiles + tile) * sp.rows + r;
+        // maximum of all parts, or what one of them found wrong (a negative sum)
+        float top = -INFINITY, code = -INFINITY;
+        for (int s = tid; s < plan.y; s += kThreads) {
+            const float2 v = sp.sums[slot0 + s * step];
+            top = fmaxf(top, v.x);
+            if (v.y < 0.f) code = fmaxf(code, v.y);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o)), code = fmaxf(code, __shfl_xor(code, o));
+        if (lane == 0) red[wave][0] = top, red[wave][1] = code;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, red[w][0]), code = fmaxf(code, red[w][1]);
+        const int i = sp.group.quotient(row), h = g * R + row - i * R;
+        T *const dst = static_cast<T *>(a.out) + (((size_t)b * a.n + i) * a.heads + h) * P;
+        if (a.status && g == 0 && row == 0 && tid == 0) a.status[b] = code > -INFINITY ? attn_status((int)-code) : 0;
+        if (code > -INFINITY) {
+            for (int e = tid; e < P; e += kThreads) from_f32(0.f, dst[e]);
+        } else {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            float sum = 0.f;
+            if (s0 < over) {
+#pragma unroll 4
+                for (int s = s0; s < plan.y; s += over) {
+                    const size_t slot = slot0 + s * step;
+                    const float2 w = sp.sums[slot];
+                    const float4 p = *reinterpret_cast<const float4 *>(sp.parts + slot * P + 4 * c);
+                    const float f = w.x == top ? 1.f : w.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.x - top);
+                    sum += w.y * f;
+                    v.x = fmaf(p.x, f, v.x), v.y = fmaf(p.y, f, v.y), v.z = fmaf(p.z, f, v.z), v.w = fmaf(p.w, f, v.w);
+                }
+            }
+            acc[tid] = v;
+            factor[tid] = sum;
+            __syncthreads();
+            if (tid < quads) {
+                for (int s = 1; s < over; ++s) {
+                    const float4 u = acc[s * quads + c];
+                    v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+                    sum += factor[s * quads + c];
+                }
+                from_f32(v.x / sum, dst[4 * c]), from_f32(v.y / sum, dst[4 * c + 1]);
+                from_f32(v.z / sum, dst[4 * c + 2]), from_f32(v.w / sum, dst[4 * c + 3]);
+            }
         }
         __syncthreads();
     }
-    top = ms[0].x, code = __float_as_int(ms[0].y);
-    const int i = sp.group.quotient(row), h = g * R + row - i * R;
-    T *const dst = static_cast<T *>(a.out) + (((size_t)b * a.n + i) * a.heads + h) * P;
-    if (a.status && g == 0 && row == 0 && tid == 0) a.status[b] = code == INT32_MAX ? 0 : attn_status(code);
-    if (code != INT32_MAX) {
-        for (int c = tid; c < P; c += kThreads) from_f32(0.f, dst[c]);
-        return;
-    }
-    // lanes: `quads` of four columns, the rest over pieces
-    const int quads = P / 4, over = kThreads / quads, c = tid % quads, s0 = tid / quads;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-    if (s0 < over)
-        for (int s = s0; s < count; s += over) {
-            const float2 w = sp.sums[slot(s)];
-            if (w.x == -INFINITY && w.y == 0.f) continue;          // (nothing seen: its rows were not written)
-            const float f = w.x == top ? 1.f : w.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.x - top);
-            const float4 p = *reinterpret_cast<const float4 *>(sp.parts + slot(s) * P + 4 * c);
-            sum += w.y * f;
-            v.x = fmaf(p.x, f, v.x), v.y = fmaf(p.y, f, v.y), v.z = fmaf(p.z, f, v.z), v.w = fmaf(p.w, f, v.w);
-        }
-    __syncthreads();
-    acc[tid] = v;
-    ms[tid].x = sum;
-    __syncthreads();
-    if (tid < quads) {
-        for (int s = 1; s < over; ++s) {
-            const float4 u = acc[s * quads + c];
-            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
-            sum += ms[s * quads + c].x;
-        }
-        from_f32(v.x / sum, dst[4 * c]), from_f32(v.y / sum, dst[4 * c + 1]);
-        from_f32(v.z / sum, dst[4 * c + 2]), from_f32(v.w / sum, dst[4 * c + 3]);
-    }
 }
 
-// row blocks of a workgroup: as many of 16 rows as there are, up to what the registers hold
-int blocks_of(int rows, int headdim) {
-    return rows <= 16 ? 1 : rows <= 32 || headdim > 128 ? 2 : 4;
-}
+// Rows of a workgroup, in blocks of 16, and workers: as many rows as there are, up to what the registers hold, unless the
+// keys that the table has room for would then leave CUs idle; as many workers as the chip holds workgroups at once.
+struct Shape {
+    int blocks, tiles, workers;
+    Shape(const stree_attn &a, const stree_kv &kv) {
+        const int rows = a.nnodes * (a.nheads / kv.nheads_kv);
+        const int64_t units = (int64_t)a.batch * kv.nheads_kv, most = units * (((int64_t)kv.max_pages * kv.page + kTileKeys - 1) / kTileKeys);
+        blocks = rows <= 16 ? 1 : rows <= 32 || kv.headdim > 128 ? 2 : 4;
+        while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
+        tiles = (rows + 16 * blocks - 1) / (16 * blocks);
+        const int regs = blocks * (kv.headdim <= 64 ? 64 : kv.headdim <= 128 ? 128 : 256);       // (as in StreamShape)
+        int64_t w = kChip * (regs <= 128 ? 3 : regs <= 256 ? 2 : 1) / tiles;
+        if (w < 1) w = 1;
+        workers = (int)(w < most ? w : most);
+    }
+};
 
 AttnSplit split_of(const stree_attn &a, const stree_kv &kv) {
-    const int R = a.nheads / kv.nheads_kv, rows = a.nnodes * R, tile = 16 * blocks_of(rows, kv.headdim);
+    const int R = a.nheads / kv.nheads_kv, rows = a.nnodes * R;
+    const Shape shape(a, kv);
     AttnSplit s(R);
-    s.tiles = (rows + tile - 1) / tile;
-    s.rows = rows < tile ? rows : tile;
-    const int64_t heads = (int64_t)a.batch * kv.nheads_kv, most = ((int64_t)kv.max_pages * kv.page + kPieceKeys - 1) / kPieceKeys;
-    int64_t want = (kWorkgroups + heads * s.tiles - 1) / (heads * s.tiles);
-    if (want > most) want = most;
-    s.pieces = (int)want;
-    s.units = 0;
+    s.workers = shape.workers;
+    s.tiles = shape.tiles;
+    s.rows = rows < 16 * shape.blocks ? rows : 16 * shape.blocks;
+    s.batch = a.batch;
+    s.plan = nullptr, s.sums = nullptr, s.parts = nullptr;
     return s;
+}
+
+// scratch: plan, sums, parts, each on 16 bytes; none where every unit has one tile
+size_t lay_out(AttnSplit &s, const stree_attn &a, const stree_kv &kv, void *workspace) {
+    if ((int64_t)kv.max_pages * kv.page <= kTileKeys) return 0;
+    const size_t units = (size_t)a.batch * kv.nheads_kv, slots = (units + s.workers) * s.tiles * s.rows;
+    const size_t plan = (units * sizeof(int2) + 15) / 16 * 16, sums = (slots * sizeof(float2) + 15) / 16 * 16;
+    char *at = static_cast<char *>(workspace);
+    s.plan = reinterpret_cast<int2 *>(at);
+    s.sums = reinterpret_cast<float2 *>(at + plan);
+    s.parts = reinterpret_cast<float *>(at + plan + sums);
+    return plan + sums + slots * kv.headdim * sizeof(float);
 }
 
 template <typename T, int PP, int MB>
 void launch_stream(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, hipStream_t st) {
-    const unsigned grid = (unsigned)((sp.units + 7) / 8 * 8) * (unsigned)sp.tiles;
+    const unsigned grid = (unsigned)((sp.workers + 7) / 8 * 8) * (unsigned)sp.tiles;
     if (kv.dim == PP) hipLaunchKernelGGL((attn_stream_kernel<T, PP, MB, true>), dim3(grid), dim3(kThreads), 0, st, a, kv, sp);
     else hipLaunchKernelGGL((attn_stream_kernel<T, PP, MB, false>), dim3(grid), dim3(kThreads), 0, st, a, kv, sp);
 }
@@ -474,19 +558,18 @@ void launch_rows(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, in
 template <typename T>
 hipError_t launch(const AttnArgs &a, const stree_attn &at, const stree_kv &kv, void *workspace, hipStream_t st) {
     AttnSplit sp = split_of(at, kv);
-    const int R = at.nheads / kv.nheads_kv, blocks = blocks_of(at.nnodes * R, kv.headdim);
-    sp.units = at.batch * kv.nheads_kv * sp.pieces;
-    const size_t slots = (size_t)sp.units * sp.tiles * sp.rows;
-    sp.parts = static_cast<float *>(workspace);
-    sp.sums = reinterpret_cast<float2 *>(sp.parts + slots * kv.headdim);
+    const bool cut = lay_out(sp, at, kv, workspace) > 0;
+    const int blocks = Shape(at, kv).blocks, rows = at.nnodes * sp.group.d, units = at.batch * kv.nheads_kv;
     const KvView<T> view(kv);
     if (kv.headdim <= 64) launch_rows<T, 64>(a, view, sp, blocks, st);
     else if (kv.headdim <= 128) launch_rows<T, 128>(a, view, sp, blocks, st);
     else launch_rows<T, 256>(a, view, sp, blocks, st);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || sp.pieces == 1) return e;
-    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(at.nnodes * R), (unsigned)(at.batch * kv.nheads_kv)), dim3(kThreads), 0, st, a,
-                       view, sp, 16 * blocks);
+    if (e != hipSuccess || !cut) return e;
+    // a workgroup per row where that is what fills the chip, several rows each where there are many
+    const int groups = rows * (int64_t)units <= 4 * kChip ? rows : (4 * kChip + units - 1) / units;
+    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(groups < rows ? groups : rows), (unsigned)units), dim3(kThreads), 0, st, a, view,
+                       sp, 16 * blocks);
     return hipGetLastError();
 }
 
@@ -495,17 +578,14 @@ hipError_t launch(const AttnArgs &a, const stree_attn &at, const stree_kv &kv, v
 bool attn_stream_supported(const stree_attn &a, const stree_kv &kv, const void *q, const void *out) {
     const int e = kv.io_dtype == STREE_BF16 ? 8 : 4;
     if (kv.headdim % e || a.q_stride_n % e || (((uintptr_t)q | (uintptr_t)out | (uintptr_t)kv.k | (uintptr_t)kv.v) % 16)) return false;
-    // grid dimensions: workgroups and, in the joining kernel, rows and heads
-    const AttnSplit s = split_of(a, kv);
-    const int64_t heads = (int64_t)a.batch * kv.nheads_kv, rows = (int64_t)a.nnodes * (a.nheads / kv.nheads_kv);
-    return (heads * s.pieces + 8) * s.tiles < (1 << 24) && (s.pieces == 1 || (heads < 65536 && rows < (1 << 24)));
+    // grid dimensions: workgroups, and units in the joining kernel
+    const Shape s(a, kv);
+    return ((int64_t)s.workers + 8) * s.tiles < (1 << 24) && (int64_t)a.batch * kv.nheads_kv < 65536;
 }
 
 size_t attn_stream_workspace(const stree_attn &a, const stree_kv &kv) {
-    const AttnSplit s = split_of(a, kv);
-    if (s.pieces == 1) return 0;
-    const size_t slots = (size_t)a.batch * kv.nheads_kv * s.pieces * s.tiles * s.rows;
-    return slots * (kv.headdim * sizeof(float) + sizeof(float2));
+    AttnSplit s = split_of(a, kv);
+    return lay_out(s, a, kv, nullptr);
 }
 
 hipError_t launch_attn_stream(const stree_attn &at, const stree_kv &kv, const AttnArgs &a, void *workspace, hipStream_t st) {
