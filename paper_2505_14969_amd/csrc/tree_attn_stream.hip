@@ -104,7 +104,7 @@ struct StreamShape {
     static constexpr int kRows = 16 * MB;
     static constexpr int kSlice = PP * kRows <= 2048 ? PP : 2048 / kRows;        // columns joined at a time: 32 KB of LDS
     static constexpr int kLd = kSlice + 4;
-    static constexpr int kMinWaves = PP * MB <= 128 ? 3 : PP * MB <= 256 ? 2 : 1;
+    static constexpr int kMinWaves = PP * MB <= 256 ? 2 : 1;                     // waves on a SIMD: as many registers as that leaves
 };
 
 template <typename T, int PP, int MB, bool WHOLE>
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     typedef Mma<T> M;
     typedef typename M::Frag Frag;
     typedef StreamShape<T, PP, MB> Shape;
-    constexpr int E = M::E, KB = M::KB, STEP = 16 * KB, NK = PP / (4 * E), NP = PP / 16, ROWS = Shape::kRows, SL = Shape::kSlice, LD = Shape::kLd;
+    constexpr int E = M::E, KB = M::KB, STEP = 16 * KB, NK = PP / (4 * E), NP = PP / 16, ROWS = Shape::kRows, STRIDE = kWaves * STEP, SL = Shape::kSlice, LD = Shape::kLd;
     struct Index { TreeLds tree; uint32_t bits[kMaxNodes * kMaxWords]; };
     __shared__ union { Index index; float o[kWaves][ROWS][LD]; int64_t first[kThreads + 1]; } lds;
     __shared__ float ml[kWaves][ROWS][2];
@@ -149,19 +149,28 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
         kp = kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + ktok) & mask) * P + grp * E;
         vp = kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)vrow << shift) + ((t + vtok) & mask);
     };
+    // Pages of up to 64 bytes a row of V come in whole lines, once: with the streaming hint.  Larger pages have the values of
+    // several steps in a line, and without the hint the next wave finds it in L2.
     auto load_k = [&](int grp) {
+        auto from = [&](int x, int c) { return reinterpret_cast<const uint4 *>(kp + 4 * x * P + (WHOLE || (4 * c + grp) * E < P ? 4 * c * E : -grp * E)); };
+        if (lines) {
+            asm volatile("; whole lines");             // (the two kinds of loads are not to be made one)
 #pragma unroll
-        for (int x = 0; x < KB; ++x)
+            for (int x = 0; x < KB; ++x)
 #pragma unroll
-            for (int c = 0; c < NK; ++c)
-                kf[x][c] = __builtin_bit_cast(Frag, *reinterpret_cast<const uint4 *>(kp + 4 * x * P + (WHOLE || (4 * c + grp) * E < P ? 4 * c * E : -grp * E)));
+                for (int c = 0; c < NK; ++c) kf[x][c] = __builtin_bit_cast(Frag, load_stream16(from(x, c)));
+            asm volatile("; whole lines");
+        } else {
+#pragma unroll
+            for (int x = 0; x < KB; ++x)
+#pragma unroll
+                for (int c = 0; c < NK; ++c) kf[x][c] = __builtin_bit_cast(Frag, *from(x, c));
+        }
     };
-    // Values of a page of up to 64 bytes a row come in whole lines, once: with the streaming hint.  Larger pages have the values
-    // of several steps in a line, and a line of keys is asked for twice: without it.
     auto load_v = [&](int col) {
         auto from = [&](int p) { return reinterpret_cast<const uint4 *>(vp + (WHOLE || 16 * p + col < P ? (size_t)(16 * p) << shift : (size_t)0)); };
         if (lines) {
-            asm volatile("; whole lines");             // (the two kinds of loads are not to be made one)
+            asm volatile("; whole lines");
 #pragma unroll
             for (int p = 0; p < NP; ++p) vf[p] = __builtin_bit_cast(Frag, load_stream16(from(p)));
             asm volatile("; whole lines");
@@ -222,7 +231,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
 #pragma unroll
             for (int p = 0; p < NP; ++p) o[mb][p] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
-        for (int t = k0 + wave * STEP; t < w1; t += kWaves * STEP) {
+        for (int t = k0 + wave * STEP; t < w1; t += STRIDE) {
             floatx4 s[MB][KB];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
@@ -233,9 +242,9 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                     for (int c = 0; c < NK; ++c) s[mb][x] = M::qk(kf[x][c], q[mb][c], s[mb][x]);
                 }
             __builtin_amdgcn_sched_barrier(0);         // (the next keys take these keys' registers, not others)
-            const bool more = t + kWaves * STEP < w1;
+            const bool more = t + STRIDE < w1;
             if (more) {
-                place(t + kWaves * STEP, col, grp);
+                place(t + STRIDE, col, grp);
                 load_k(grp);
             }
             const bool tail = t + STEP > len || t + STEP > w1;
@@ -511,7 +520,7 @@ struct Shape {
         while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
         tiles = (rows + 16 * blocks - 1) / (16 * blocks);
         const int regs = blocks * (kv.headdim <= 64 ? 64 : kv.headdim <= 128 ? 128 : 256);       // (as in StreamShape)
-        int64_t w = kChip * (regs <= 128 ? 3 : regs <= 256 ? 2 : 1) / tiles;
+        int64_t w = kChip * (regs <= 256 ? 2 : 1) / tiles;
         if (w < 1) w = 1;
         workers = (int)(w < most ? w : most);
     }
