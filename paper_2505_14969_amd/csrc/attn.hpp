@@ -77,9 +77,9 @@ struct Share {
     int64_t x;
     Shares shares;
 
-    // Finds the worker's first tile; the whole workgroup calls it (`first`: kThreads numbers of LDS, free again behind the next
+    // Finds the worker's first tile; the whole workgroup calls it (`first`: a number of LDS for every thread, free again behind the next
     // barrier).  Up to 64 sequences each wave finds it by itself.
-    template <typename T>
+    template <int THREADS = kThreads, typename T>
     __device__ __forceinline__ static Share start(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, int worker, int64_t *first) {
         const int lane = threadIdx.x & 63;
         if (sp.batch <= 64) {
@@ -99,7 +99,7 @@ struct Share {
             return s;
         }
         // tiles in front of every run of sequences, one run a thread
-        const int run = (sp.batch + kThreads - 1) / kThreads, wave = threadIdx.x >> 6;
+        const int run = (sp.batch + THREADS - 1) / THREADS, wave = threadIdx.x >> 6;
         int64_t sum = 0;
         for (int y = threadIdx.x * run; y < min((int)(threadIdx.x + 1) * run, sp.batch); ++y) sum += tiles_of(kv, a.lengths[y], a.n);
         const int64_t mine = sum;
@@ -112,7 +112,7 @@ struct Share {
         __syncthreads();
         int64_t total = 0;
 #pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             const int64_t u = first[w];
             if (w < wave) sum += u;
             total += u;
@@ -123,7 +123,7 @@ struct Share {
         Share s(Shares(uniform(total) * kv.heads, sp.workers));
         if (worker >= s.workers) return s;
         s.x = s.shares.begin(worker);
-        int lo = 0, hi = kThreads;
+        int lo = 0, hi = THREADS;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (first[mid] * kv.heads <= s.x) lo = mid;
@@ -164,6 +164,56 @@ struct Share {
     }
 };
 
+// Numbers of the pages that a wave walks over, 64 at a time in its lanes and the next 64 on their way.
+template <typename T>
+struct PageWalk {
+    int cur, next, first;
+    bool bad;
+    __device__ __forceinline__ int window(const KvView<T> &kv, int b, int j0, int end, int lane) {
+        const int j = j0 + lane;
+        int pg = 0;
+        if (j < end) {
+            pg = kv.table[(size_t)b * kv.max_pages + j];
+            if (!kv.exists(pg)) bad = true, pg = 0;
+        }
+        return pg;
+    }
+    __device__ __forceinline__ void start(const KvView<T> &kv, int b, int j0, int end, int lane) {
+        bad = false;
+        first = j0;
+        cur = window(kv, b, j0, end, lane);
+        next = window(kv, b, j0 + 64, end, lane);
+    }
+    // pages from j on (j grows from call to call by less than 64)
+    __device__ __forceinline__ void reach(const KvView<T> &kv, int b, int j, int end, int lane) {
+        if (j - first >= 64) {
+            first += 64;
+            cur = next;
+            next = window(kv, b, first + 64, end, lane);
+        }
+    }
+    __device__ __forceinline__ int at(int j) const {
+        const int r = j - first;
+        return r < 64 ? __builtin_amdgcn_readlane(cur, r) : __builtin_amdgcn_readlane(next, r - 64);
+    }
+};
+
+// Which of E consecutive nodes from j0 on (negative: text) node i sees, bit by bit.
+template <int E>
+__device__ __forceinline__ uint32_t seen_nodes(const uint32_t *bits, int words, bool tree, int i, int j0) {
+    constexpr uint32_t kAll = (1u << E) - 1u;
+    if (!tree) {
+        const int c = min(max(i - j0 + 1, 0), E);
+        return (1u << c) - 1u;
+    }
+    if (j0 <= -E) return kAll;
+    const int w = j0 >> 5;
+    const uint32_t lo = w >= 0 && w < words ? bits[i * words + w] : 0u, hi = w + 1 < words ? bits[i * words + w + 1] : 0u;
+    uint32_t v = (uint32_t)((((unsigned long long)hi << 32) | lo) >> (j0 & 31));
+    if (j0 < 0) v |= (1u << -j0) - 1u;
+    return v & kAll;
+}
+
 // What is wrong with a sequence as a small positive number, the first bad node before a page (two pieces may find both).
 __device__ __forceinline__ int attn_code(int status) { return status > 0 ? status : 1000; }
 __device__ __forceinline__ int attn_status(int code) { return code < 1000 ? code : STREE_SEQ_PAGE; }
@@ -171,6 +221,7 @@ __device__ __forceinline__ int attn_status(int code) { return code < 1000 ? code
 // the streaming kernel (tree_attn_stream.hip)
 bool attn_stream_supported(const stree_attn &a, const stree_kv &kv, const void *q, const void *out);
 size_t attn_stream_workspace(const stree_attn &a, const stree_kv &kv);
+hipError_t launch_attn_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, int rows, hipStream_t st);   // (tree_attn_tile.hip)
 hipError_t launch_attn_stream(const stree_attn &at, const stree_kv &kv, const AttnArgs &a, void *workspace, hipStream_t st);
 
 }  // namespace stree

@@ -49,56 +49,6 @@ struct Mma<float> {
     static __device__ __forceinline__ Frag round(const float (&p)[4]) { return Frag{p[0], p[1], p[2], p[3]}; }
 };
 
-// Numbers of the pages that a wave walks over, 64 at a time in its lanes and the next 64 on their way.
-template <typename T>
-struct PageWalk {
-    int cur, next, first;
-    bool bad;
-    __device__ __forceinline__ int window(const KvView<T> &kv, int b, int j0, int end, int lane) {
-        const int j = j0 + lane;
-        int pg = 0;
-        if (j < end) {
-            pg = kv.table[(size_t)b * kv.max_pages + j];
-            if (!kv.exists(pg)) bad = true, pg = 0;
-        }
-        return pg;
-    }
-    __device__ __forceinline__ void start(const KvView<T> &kv, int b, int j0, int end, int lane) {
-        bad = false;
-        first = j0;
-        cur = window(kv, b, j0, end, lane);
-        next = window(kv, b, j0 + 64, end, lane);
-    }
-    // pages from j on (j grows from call to call by less than 64)
-    __device__ __forceinline__ void reach(const KvView<T> &kv, int b, int j, int end, int lane) {
-        if (j - first >= 64) {
-            first += 64;
-            cur = next;
-            next = window(kv, b, first + 64, end, lane);
-        }
-    }
-    __device__ __forceinline__ int at(int j) const {
-        const int r = j - first;
-        return r < 64 ? __builtin_amdgcn_readlane(cur, r) : __builtin_amdgcn_readlane(next, r - 64);
-    }
-};
-
-// Which of E consecutive nodes from j0 on (negative: text) node i sees, bit by bit.
-template <int E>
-__device__ __forceinline__ uint32_t seen_nodes(const uint32_t *bits, int words, bool tree, int i, int j0) {
-    constexpr uint32_t kAll = (1u << E) - 1u;
-    if (!tree) {
-        const int c = min(max(i - j0 + 1, 0), E);
-        return (1u << c) - 1u;
-    }
-    if (j0 <= -E) return kAll;
-    const int w = j0 >> 5;
-    const uint32_t lo = w >= 0 && w < words ? bits[i * words + w] : 0u, hi = w + 1 < words ? bits[i * words + w + 1] : 0u;
-    uint32_t v = (uint32_t)((((unsigned long long)hi << 32) | lo) >> (j0 & 31));
-    if (j0 < 0) v |= (1u << -j0) - 1u;
-    return v & kAll;
-}
-
 template <typename T, int PP, int MB>
 struct StreamShape {
     static constexpr int kRows = 16 * MB;
@@ -513,9 +463,18 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
 // keys that the table has room for would then leave CUs idle; as many workers as the chip holds workgroups at once.
 struct Shape {
     int blocks, tiles, workers;
+    bool shared;                                     // the kernel that shares tiles of keys through LDS
     Shape(const stree_attn &a, const stree_kv &kv) {
         const int rows = a.nnodes * (a.nheads / kv.nheads_kv);
         const int64_t units = (int64_t)a.batch * kv.nheads_kv, most = units * (((int64_t)kv.max_pages * kv.page + kTileKeys - 1) / kTileKeys);
+        shared = kv.io_dtype == STREE_BF16 && (kv.headdim == 64 || kv.headdim == 128) && rows > 64;
+        if (shared) {
+            blocks = rows <= 128 ? 8 : 16;
+            tiles = (rows + 16 * blocks - 1) / (16 * blocks);
+            const int w = kChip / tiles < 1 ? 1 : kChip / tiles;
+            workers = (int)(w < most ? w : most);
+            return;
+        }
         blocks = rows <= 16 ? 1 : rows <= 32 || kv.headdim > 128 ? 2 : 4;
         while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
         tiles = (rows + 16 * blocks - 1) / (16 * blocks);
@@ -568,12 +527,18 @@ template <typename T>
 hipError_t launch(const AttnArgs &a, const stree_attn &at, const stree_kv &kv, void *workspace, hipStream_t st) {
     AttnSplit sp = split_of(at, kv);
     const bool cut = lay_out(sp, at, kv, workspace) > 0;
-    const int blocks = Shape(at, kv).blocks, rows = at.nnodes * sp.group.d, units = at.batch * kv.nheads_kv;
+    const Shape shape(at, kv);
+    const int blocks = shape.blocks, rows = at.nnodes * sp.group.d, units = at.batch * kv.nheads_kv;
     const KvView<T> view(kv);
-    if (kv.headdim <= 64) launch_rows<T, 64>(a, view, sp, blocks, st);
+    hipError_t e;
+    if (shape.shared) {
+        e = launch_attn_tile(a, kv, sp, 16 * blocks, st);
+        if (e != hipSuccess) return e;
+    }
+    else if (kv.headdim <= 64) launch_rows<T, 64>(a, view, sp, blocks, st);
     else if (kv.headdim <= 128) launch_rows<T, 128>(a, view, sp, blocks, st);
     else launch_rows<T, 256>(a, view, sp, blocks, st);
-    hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess || !cut) return e;
     // a workgroup per row where that is what fills the chip, several rows each where there are many
     const int groups = rows * (int64_t)units <= 4 * kChip ? rows : (4 * kChip + units - 1) / units;

@@ -1,0 +1,354 @@
+// The kernel of stree_tree_attn for many query rows: 128 or 256 rows (node, head) of one key/value head share every tile of
+// 64 keys through LDS, products on the bf16 matrix units.
+//
+// With 256 rows a key of 512 bytes comes with 131072 operations: memory and the matrix units need about the same time, and the
+// exponentials (a quarter of the vector rate) nearly as much again, so everything has to overlap: eight waves, two on a SIMD,
+// of 32 rows each.  (64 rows a wave would halve the operands read from LDS, which need as long as the products; but with 256
+// values in accumulators the compiler spills what is on its way from memory: 199 us where this takes FIGURE.)  As in the streaming kernel a lane owns a query row in every
+// accumulator (S^T = K Q^T, O^T += V^T P^T), keys stand in S^T in the order that makes the probabilities the operand of the
+// second product, and the maximum moves only when a score passes it by kSlack.  Tiles go through registers into two LDS
+// buffers, the next one's loads in flight behind the products: one barrier a tile.
+#include "attn.hpp"
+
+namespace stree {
+
+namespace {
+
+constexpr float kSlack = 8.f;
+constexpr int kKeys = 64;                            // keys of a tile
+constexpr int kTileThreads = 512;
+
+// Rows of K are 16-byte pieces, permuted by the key, so that eight lanes that read the same piece of keys that follow one
+// another in S^T use all banks; 16 tokens of V are rows of 32 bytes, whose halves change places every four rows.
+template <int PP, int RW>
+struct TileLds {
+    static constexpr int kTile = kKeys * PP;         // elements
+    bf16_t k[2][kTile], v[2][kTile];
+    uint32_t bits[kMaxNodes * kMaxWords];
+};
+
+template <int PP, int RW>
+__global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, KvView<bf16_t> kv, AttnSplit sp) {
+    constexpr int ROWS = 32 * RW, KW = 8 / RW, KB = 2 / KW, NC = PP / 16, NPB = PP / 32;    // key waves; blocks of 32 keys a wave
+    constexpr int PIECES = kKeys * PP / 8 / kTileThreads;                                     // 16-byte pieces of a tile per thread
+    static_assert(KW * KB == 2, "64 keys a tile");
+    typedef TileLds<PP, RW> Lds;
+    __shared__ Lds lds;
+    __shared__ float ml[KW > 1 ? ROWS : 1][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wr = wave % RW, wk = wave / RW;
+    const int col = lane & 31, half = lane >> 5;
+    const int tile = (int)(blockIdx.x >> 3) % sp.tiles, worker = ((int)(blockIdx.x >> 3) / sp.tiles) * 8 + (int)(blockIdx.x & 7);
+    if (worker >= sp.workers) return;
+    const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, words = (a.n + 31) / 32;
+    bf16_t *const out = static_cast<bf16_t *>(a.out);
+    Share at = Share::start<kTileThreads>(a, kv, sp, worker, reinterpret_cast<int64_t *>(lds.k[0]));
+    if (worker >= at.workers) return;
+    __syncthreads();                                   // (its numbers lay where the first tile goes)
+
+    // where a thread's pieces of a tile lie: K by rows, V by runs of 16 tokens
+    const int shift = kv.shift, mask = kv.mask();
+    const size_t block = (size_t)PP << shift;
+    constexpr int KR = PP / 8, KSTEP = kTileThreads / KR;                 // pieces of a row of K; rows a pass
+    const int krow = tid / KR, kpiece = tid % KR;
+    constexpr int VP = 2 * PP, VSTEP = kTileThreads / VP;    // pieces of 16 tokens of V; such runs a pass
+    const int vrun = tid / VP, vrow = tid % VP >> 1, vhalf = tid & 1;
+    const int kput = krow * PP + ((kpiece ^ ((krow & 3) | ((krow >> 1) & 4))) * 8);
+    const int vput = vrun * 16 * PP + vrow * 16 + ((vhalf ^ ((vrow >> 2) & 1)) * 8);
+    // where a lane's operands lie
+    const int ktok = (col & 3) | ((col >> 1) & 4) | ((col << 1) & 8) | (col & 16);      // S^T row -> key
+    // (row r = 4 h + e of a block of 16 holds key 8 h + e, row 8 + 4 h + e key 8 h + 4 + e)
+    const int kx = half ^ ((ktok & 3) | ((ktok >> 1) & 4));
+    int kget[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) kget[c] = ktok * PP + ((2 * c) ^ kx) * 8;
+    const int vget = col * 16 + (half ^ ((col >> 2) & 1)) * 8;
+
+    int k0 = 0, k1 = 0, whole = 0, end = 0;
+    PageWalk<bf16_t> walk;
+    bf16x8 q[NC];
+    bf16x8 sk[PIECES], sv[PIECES];
+    auto fetch = [&](int t) {                          // a tile's pieces on their way
+        walk.reach(kv, at.b, t >> shift, end, lane);
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x) {
+            const int tk = t + ((x * KSTEP + krow) & ~15), pk = walk.at(uniform(min(tk >> shift, end - 1)));
+            sk[x] = *reinterpret_cast<const bf16x8 *>(kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + x * KSTEP + krow) & mask) * PP + kpiece * 8);
+            const int tv = t + 16 * (x * VSTEP + vrun), pv = walk.at(uniform(min(tv >> shift, end - 1)));
+            sv[x] = *reinterpret_cast<const bf16x8 *>(kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)vrow << shift) + (tv & mask) + vhalf * 8);
+        }
+    };
+    auto enter = [&]() {
+        const int lane2 = again(lane), col = lane2 & 31, half = lane2 >> 5;
+        k0 = k1 = whole = 0;
+        if (at.len >= 0 && kv.fits((int64_t)at.len + a.n)) {
+            const int last = sp.group.quotient(min(row0 + ROWS, rows) - 1);
+            k0 = at.t0 * kTileKeys, whole = min(at.t1 * kTileKeys, at.len + a.n);
+            k1 = min(whole, at.len + last + 1);
+        }
+        walk.bad = false;
+        if (k0 >= k1) return;
+        end = ((k1 - 1) >> shift) + 1;
+        walk.start(kv, at.b, k0 >> shift, end, lane);
+            {
+            const int r = row0 + wr * 32 + col, rr = min(r, rows - 1), i = sp.group.quotient(rr), h = at.g * R + rr - i * R;
+            const bf16_t *src = static_cast<const bf16_t *>(a.q) + ((size_t)at.b * a.n + i) * a.q_sn + (size_t)h * PP + half * 8;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) q[c] = *reinterpret_cast<const bf16x8 *>(src + c * 16);
+        }
+        fetch(k0);
+    };
+    enter();
+    for (;;) {
+        const int b = at.b, g = at.g, len = at.len, w1 = k1, unit = b * kv.heads + g;
+        const bool direct = at.whole();
+        if (at.t0 == 0 && sp.plan && tile == 0 && tid == 0)
+            sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
+        int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
+        if (whole > len && len >= 0 && whole > 0 && a.parent) {
+            __syncthreads();                           // (the index borrows a tile's place)
+            bad = index_nodes(*reinterpret_cast<TreeLds *>(lds.v[0]), lds.bits, a.parent, b, a.n, words);
+            __syncthreads();
+        }
+        const int col = again(lane) & 31, half = again(lane) >> 5;
+        float m, base, l;
+        floatx16 o[NPB];
+        int node;
+            {
+            node = sp.group.quotient(min(row0 + wr * 32 + col, rows - 1));
+            m = -INFINITY, base = 0.f, l = 0.f;
+#pragma unroll
+            for (int p = 0; p < NPB; ++p)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
+        }
+        int buf = 0;
+        for (int t = k0; t < w1; t += kKeys, buf ^= 1) {
+            const bool tail = t + kKeys > len || t + kKeys > w1;
+            // Values behind the last node are no numbers anybody wrote.
+            int odd = 0;
+            if (tail) {
+#pragma unroll
+                for (int x = 0; x < PIECES; ++x) {
+                    const int left = len + a.n - (t + 16 * (x * VSTEP + vrun) + vhalf * 8);
+                    bf16x8 f = sv[x];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (e >= left) f[e] = (bf16_t)0.f;
+                        odd |= !(fabsf((float)f[e]) < INFINITY);
+                    }
+                    sv[x] = f;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) {
+                *reinterpret_cast<bf16x8 *>(&lds.k[buf][kput + x * KSTEP * PP]) = sk[x];
+                *reinterpret_cast<bf16x8 *>(&lds.v[buf][vput + x * VSTEP * 16 * PP]) = sv[x];
+            }
+            if (tail) odd = __syncthreads_or(odd);
+            else __syncthreads();
+            if (t + kKeys < w1) fetch(t + kKeys);
+
+            const bf16_t *const kt = lds.k[buf] + wk * 32 * PP, *const vt = lds.v[buf] + wk * 32 * PP;
+            uint32_t seen[KB];                      // 16 keys a block and lane: bits 0 - 7 of its first 16, 8 - 15 of its last
+            if (__builtin_expect(tail, 0)) {
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        seen[kb] = 0;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int t8 = t + (wk * KB + kb) * 32 + y * 16 + half * 8, left = w1 - t8;
+                            uint32_t v = seen_nodes<8>(lds.bits, words, a.parent != nullptr, node, t8 - len);
+                            v &= left >= 8 ? 0xffu : left > 0 ? (1u << left) - 1u : 0u;
+                            seen[kb] |= v << (8 * y);
+                        }
+                    }
+                if (__builtin_expect(odd, 0)) {
+                    // Infinities and NaN among the values of nodes: zero probabilities would not keep them from the rows that do
+                    // not see the node.  They are counted per row, and are zeros for the products below.
+#pragma unroll 1
+                    for (int y = 0; y < 2 * KB; ++y) {
+                        const int kb = y >> 1;
+#pragma unroll
+                        for (int p = 0; p < NPB; ++p) {
+                            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(vt + y * 16 * PP + vget + p * 32 * 16);
+                            bf16x8 up, down;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                up[e] = (bf16_t)((float)v[e] < INFINITY ? 0.f : 1.f);              // +inf, NaN
+                                down[e] = (bf16_t)((float)v[e] > -INFINITY ? 0.f : 1.f);           // -inf, NaN
+                            }
+            {
+                                const uint32_t bits = (KB > 1 && kb ? seen[KB - 1] : seen[0]) >> (8 * (y & 1));
+                                bf16x8 see;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) see[e] = (bf16_t)((bits >> e) & 1u ? 1.f : 0.f);
+                                floatx16 cu, cd;
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) cu[e] = cd[e] = 0.f;
+                                cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, see, cu, 0, 0, 0);
+                                cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, see, cd, 0, 0, 0);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    if (cu[e] > 0.f) o[p][e] += INFINITY;
+                                    if (cd[e] > 0.f) o[p][e] -= INFINITY;
+                                }
+                            }
+                        }
+                    }
+                    __syncthreads();
+                    for (int x = tid; x < kKeys * PP; x += kTileThreads)
+                        if (!(fabsf((float)lds.v[buf][x]) < INFINITY)) lds.v[buf][x] = (bf16_t)0.f;
+                    __syncthreads();
+                }
+            }
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {          // 32 keys
+                floatx16 s;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kt + kget[c & 3] + (c >> 2) * 64 + kb * 32 * PP);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s, 0, 0, 0);
+                }
+                if (__builtin_expect(tail, 0)) {
+                    // (a negative scale turns the order: no score at all is +infinity then)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (!((seen[kb] >> e) & 1u)) s[e] = a.scale < 0.f ? INFINITY : -INFINITY;
+                }
+                bool above = false;
+                float top;
+            {
+                    float hi = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) hi = fmaxf(hi, s[e] * a.scale);
+                    top = hi;
+                    above |= hi > m + kSlack;
+                }
+                if (__builtin_expect(__any(above), 0)) {
+            {
+                        const float v = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                        const float b2 = v == -INFINITY ? 0.f : v, keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - b2);
+                        m = v, base = b2;
+                        l *= keep;
+#pragma unroll
+                        for (int p = 0; p < NPB; ++p) o[p] *= keep;
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    bf16x8 pf;
+            {
+                        // one rounding of each probability; their sum is the rounded ones'
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[8 * y + e], a.scale, -base));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) l += (float)pf[e];
+                    }
+#pragma unroll
+                    for (int p = 0; p < NPB; ++p) {
+                        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(vt + (2 * kb + y) * 16 * PP + vget + p * 32 * 16);
+                        o[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf, o[p], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        // (pages of the piece that only later rows see)
+        int missing = walk.bad;
+        for (int j = (k1 >> shift) + tid; j < (whole + mask) >> shift; j += kTileThreads) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
+        if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
+        const bool more = at.next(a, kv);
+        if (more) enter();                             // the next piece's first tile is on its way
+
+        {
+        const int lane2 = again(lane), col = lane2 & 31, half = lane2 >> 5;
+        const bool dead = len < 0 || bad != 0;
+        const size_t slot = ((size_t)(worker + unit) * sp.tiles + tile) * sp.rows;
+        l += __shfl_xor(l, 32);
+        if constexpr (KW > 1) {
+            // the second half of the keys is handed to the first's waves, 32 rows at a time: [wave][p][row]
+            float *const give = reinterpret_cast<float *>(lds.k[0]) + wr * (PP * 32);
+            static_assert(RW * PP * 32 * sizeof(float) <= sizeof(lds.k) + sizeof(lds.v), "room for it");
+            {
+                const int r = wr * 32 + col;
+                if (wk == 1) {
+                    if (half == 0) ml[r][0] = m, ml[r][1] = l;
+#pragma unroll
+                    for (int p = 0; p < NPB; ++p)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] = o[p][e];
+                }
+                __syncthreads();
+                if (wk == 0) {
+                    const float m2 = ml[r][0], hi = fmaxf(m, m2);
+                    // (rows without a finite score: their sums stay what they are)
+                    const float f1 = m == hi ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - hi);
+                    const float f2 = m2 == hi ? 1.f : m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - hi);
+                    m = hi;
+                    l = l * f1 + ml[r][1] * f2;
+#pragma unroll
+                    for (int p = 0; p < NPB; ++p)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[p][e] = o[p][e] * f1 + give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] * f2;
+                }
+                __syncthreads();
+            }
+        }
+        // The results turned round in LDS, half of the columns at a time: a lane's row becomes runs of 16-byte pieces of rows.
+        constexpr int QS = PP / 8;                     // pieces of four columns of half a row
+        float *const turn = reinterpret_cast<float *>(lds.k[0]) + wr * (32 * PP / 2);
+        static_assert(RW * 16 * PP * sizeof(float) <= sizeof(lds.k) + sizeof(lds.v), "room for it");
+        if (wk == 0) {
+            const int r0 = row0 + wr * 32;
+            const float by = !direct ? 1.f : dead ? 0.f : 1.f / l;
+            if (!direct && half == 0 && r0 + col < rows) sp.sums[slot + wr * 32 + col] = make_float2(m, bad ? -(float)attn_code(bad) : l);
+#pragma unroll
+            for (int hp = 0; hp < 2; ++hp) {
+#pragma unroll
+                for (int p = 0; p < NPB / 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const floatx16 &v = o[hp * (NPB / 2) + p];
+                        const int piece = p * 8 + e / 2 + half;
+                        *reinterpret_cast<float4 *>(turn + (col * QS + (piece ^ (col & (QS - 1)))) * 4) = make_float4(v[e] * by, v[e + 1] * by, v[e + 2] * by, v[e + 3] * by);
+                    }
+                wave_sync();
+#pragma unroll
+                for (int x = 0; x < 32 * QS / 64; ++x) {
+                    const int y = x * 64 + lane2, r = y / QS, piece = y % QS, row = r0 + r;
+                    const float4 v = *reinterpret_cast<const float4 *>(turn + (r * QS + (piece ^ (r & (QS - 1)))) * 4);
+                    const int c = hp * (PP / 2) + piece * 4;
+                    if (row >= rows) continue;
+                    if (direct) {
+                        const int i = sp.group.quotient(row), h = g * R + row - i * R;
+                        *reinterpret_cast<uint2 *>(out + (((size_t)b * a.n + i) * a.heads + h) * PP + c) = dead ? make_uint2(0u, 0u) : pack_bf16x4(v.x, v.y, v.z, v.w);
+                    } else if (!dead) {
+                        *reinterpret_cast<float4 *>(sp.parts + (slot + wr * 32 + r) * PP + c) = v;
+                    }
+                }
+                wave_sync();
+            }
+        }
+        }
+        if (direct && a.status && g == 0 && tile == 0 && tid == 0) a.status[b] = bad;
+        if (!more) break;
+        __syncthreads();                               // (LDS is read)
+    }
+}
+
+template <int PP, int RW>
+void launch_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, hipStream_t st) {
+    const unsigned grid = (unsigned)((sp.workers + 7) / 8 * 8) * (unsigned)sp.tiles;
+    hipLaunchKernelGGL((attn_tile_kernel<PP, RW>), dim3(grid), dim3(kTileThreads), 0, st, a, KvView<bf16_t>(kv), sp);
+}
+
+}  // namespace
+
+hipError_t launch_attn_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, int rows, hipStream_t st) {
+    if (kv.headdim == 64) rows == 128 ? launch_tile<64, 4>(a, kv, sp, st) : launch_tile<64, 8>(a, kv, sp, st);
+    else rows == 128 ? launch_tile<128, 4>(a, kv, sp, st) : launch_tile<128, 8>(a, kv, sp, st);
+    return hipGetLastError();
+}
+
+}  // namespace stree
