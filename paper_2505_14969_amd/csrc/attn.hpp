@@ -15,6 +15,22 @@ struct AttnArgs {
     float scale;                       // of <q, k>, in units of log2(e): probabilities are powers of two
 };
 
+// Queries as a matrix operand: the sign of the scale is theirs, so that the largest product is the largest score.
+template <typename Frag>
+__device__ __forceinline__ Frag signed_query(Frag q, float scale) { return scale < 0.f ? -q : q; }
+
+// sum + the values of a bf16 operand
+__device__ __forceinline__ float sum_of(bf16x8 v, float sum) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const uint4 u = __builtin_bit_cast(uint4, v);
+    const bf16x2_t one = {(__bf16)1.f, (__bf16)1.f};
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u.x), one, sum, false);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u.y), one, sum, false);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u.z), one, sum, false);
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u.w), one, sum, false);
+}
+__device__ __forceinline__ float sum_of(floatx4 v, float sum) { return sum + ((v[0] + v[1]) + (v[2] + v[3])); }
+
 constexpr int kTileKeys = 128;         // keys that the work is counted in: a step of bf16 keys for each of four waves
 
 // The work of a call is B sequences x heads x tiles of their keys, which the device alone knows how many there are of: every

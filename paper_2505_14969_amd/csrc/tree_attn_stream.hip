@@ -72,6 +72,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     if (worker >= sp.workers) return;
     const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, mine = min(ROWS, rows - row0);
     T *const out = static_cast<T *>(a.out);
+    const float scale = fabsf(a.scale);
     Share at = Share::start(a, kv, sp, worker, lds.first);
     if (worker >= at.workers) return;
 
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 const int x = (4 * c + grp) * E;
                 const bool there = r < rows && x < P;
                 const uint4 v = *reinterpret_cast<const uint4 *>(src + (there ? x : 0));
-                q[mb][c] = __builtin_bit_cast(Frag, there ? v : make_uint4(0u, 0u, 0u, 0u));
+                q[mb][c] = signed_query(__builtin_bit_cast(Frag, there ? v : make_uint4(0u, 0u, 0u, 0u)), a.scale);
             }
         }
         place(t, col, grp);
@@ -211,11 +212,12 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 }
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    float v = s[mb][e >> 2][e & 3] * a.scale;
+                    float v = s[mb][e >> 2][e & 3];
                     if (tail && !((seen[mb] >> e) & 1u)) v = -INFINITY;
                     p[mb][e] = v;
                     top[mb] = fmaxf(top[mb], v);
                 }
+                top[mb] *= scale;
                 above |= top[mb] > m[mb] + kSlack;
             }
             if (__builtin_expect(__any(above), 0)) {
@@ -276,10 +278,9 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) p[mb][e] = __builtin_amdgcn_exp2f(p[mb][e] - base[mb]);
+                for (int e = 0; e < E; ++e) p[mb][e] = __builtin_amdgcn_exp2f(fmaf(p[mb][e], scale, -base[mb]));
                 const Frag pf = M::round(p[mb]);       // bf16: one rounding of each probability, and their sum is the rounded ones'
-#pragma unroll
-                for (int e = 0; e < E; ++e) l[mb] += (float)pf[e];
+                l[mb] = sum_of(pf, l[mb]);
 #pragma unroll
                 for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
             }

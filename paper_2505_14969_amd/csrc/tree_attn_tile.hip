@@ -41,6 +41,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
     if (worker >= sp.workers) return;
     const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, words = (a.n + 31) / 32;
     bf16_t *const out = static_cast<bf16_t *>(a.out);
+    const float scale = fabsf(a.scale);
     Share at = Share::start<kTileThreads>(a, kv, sp, worker, reinterpret_cast<int64_t *>(lds.k[0]));
     if (worker >= at.workers) return;
     __syncthreads();                                   // (its numbers lay where the first tile goes)
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
             const int r = row0 + wr * 32 + col, rr = min(r, rows - 1), i = sp.group.quotient(rr), h = at.g * R + rr - i * R;
             const bf16_t *src = static_cast<const bf16_t *>(a.q) + ((size_t)at.b * a.n + i) * a.q_sn + (size_t)h * PP + half * 8;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) q[c] = *reinterpret_cast<const bf16x8 *>(src + c * 16);
+            for (int c = 0; c < NC; ++c) q[c] = signed_query(*reinterpret_cast<const bf16x8 *>(src + c * 16), a.scale);
         }
         fetch(k0);
     };
@@ -205,27 +206,29 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
             for (int kb = 0; kb < KB; ++kb) {          // 32 keys
                 floatx16 s;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
+                bf16x8 kf[NC], vf[2][NPB];
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const bf16x8 k = *reinterpret_cast<const bf16x8 *>(kt + kget[c & 3] + (c >> 2) * 64 + kb * 32 * PP);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s, 0, 0, 0);
-                }
+                for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const bf16x8 *>(kt + kget[c & 3] + (c >> 2) * 64 + kb * 32 * PP);
+                __builtin_amdgcn_sched_barrier(0);     // (all operands requested before the first product, not one by one)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], s, 0, 0, 0);
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int p = 0; p < NPB; ++p) vf[y][p] = *reinterpret_cast<const bf16x8 *>(vt + (2 * kb + y) * 16 * PP + vget + p * 32 * 16);
+                __builtin_amdgcn_sched_barrier(0);
                 if (__builtin_expect(tail, 0)) {
-                    // (a negative scale turns the order: no score at all is +infinity then)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (!((seen[kb] >> e) & 1u)) s[e] = a.scale < 0.f ? INFINITY : -INFINITY;
+                    for (int e = 0; e < 16; ++e)
+                        if (!((seen[kb] >> e) & 1u)) s[e] = -INFINITY;
                 }
                 bool above = false;
-                float top;
-            {
-                    float hi = -INFINITY;
+                float top = -INFINITY;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) hi = fmaxf(hi, s[e] * a.scale);
-                    top = hi;
-                    above |= hi > m + kSlack;
-                }
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+                top *= scale;
+                above |= top > m + kSlack;
                 if (__builtin_expect(__any(above), 0)) {
             {
                         const float v = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
@@ -238,19 +241,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
                 }
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
+                    // one rounding of each probability; their sum is the rounded ones'
                     bf16x8 pf;
-            {
-                        // one rounding of each probability; their sum is the rounded ones'
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[8 * y + e], a.scale, -base));
+                    for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[8 * y + e], scale, -base));
+                    l = sum_of(pf, l);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) l += (float)pf[e];
-                    }
-#pragma unroll
-                    for (int p = 0; p < NPB; ++p) {
-                        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(vt + (2 * kb + y) * 16 * PP + vget + p * 32 * 16);
-                        o[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf, o[p], 0, 0, 0);
-                    }
+                    for (int p = 0; p < NPB; ++p) o[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[y][p], pf, o[p], 0, 0, 0);
                 }
             }
         }
