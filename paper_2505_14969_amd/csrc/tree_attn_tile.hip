@@ -4,7 +4,7 @@
 // With 256 rows a key of 512 bytes comes with 131072 operations: memory and the matrix units need about the same time, and the
 // exponentials (a quarter of the vector rate) nearly as much again, so everything has to overlap: eight waves, two on a SIMD,
 // of 32 rows each.  (64 rows a wave would halve the operands read from LDS, which need as long as the products; but with 256
-// values in accumulators the compiler spills what is on its way from memory: 199 us where this takes FIGURE.)  As in the streaming kernel a lane owns a query row in every
+// values in accumulators the compiler spills what is on its way from memory: 16 trees of 64 nodes 199 us where this takes 84.)  As in the streaming kernel a lane owns a query row in every
 // accumulator (S^T = K Q^T, O^T += V^T P^T), keys stand in S^T in the order that makes the probabilities the operand of the
 // second product, and the maximum moves only when a score passes it by kSlack.  Tiles go through registers into two LDS
 // buffers, the next one's loads in flight behind the products: one barrier a tile.

@@ -1,6 +1,6 @@
 // stree_tree_rope: per head of q and k an RMS norm and the rotation to the node's position, k and v appended to the paged cache.
 //   x^ = x / sqrt(mean x^2 + eps) * w;  pairs (u, w) turn by 2 pi frac(position * turns[j]), frac in 64 bits
-// Rows are read once and written once: bound by memory, and for a few nodes by the chain length -> tree -> angles -> rows.
+// Rows are read once and written once: bound by memory, and for a few nodes by the chain length -> tree, pages -> angles -> rows.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 
@@ -28,7 +28,7 @@ __device__ __forceinline__ float2 rotation(double turns, int position, float sca
     return make_float2(c * scale, s * scale);
 }
 
-// One workgroup per node, a wave per head: any head size, any alignment.
+// One workgroup per node, a wave per head: any head size, any alignment, any pairs.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rope_plain_kernel(RopeArgs a, KvView<T> kv) {
     __shared__ TreeLds tree;
@@ -97,10 +97,230 @@ __global__ __launch_bounds__(kThreads) void rope_plain_kernel(RopeArgs a, KvView
     }
 }
 
+// Depth of every node of a tree of at most 64 by one wave (lane = node), or first bad node + 1 (alike in all lanes).
+__device__ __forceinline__ int wave_depths(const int32_t *__restrict__ parent, int n, int lane, int &depth) {
+    int p = lane < n ? parent[lane] : -1;
+    const unsigned long long wrong = __ballot(lane < n && (lane == 0 ? p != -1 : (p < 0 || p >= lane)));
+    if (wrong) return __ffsll((long long)wrong);
+    depth = p >= 0 ? 1 : 0;
+    while (__any(p >= 0)) {                            // (at most six times: the way left is halved)
+        const int q = p >= 0 ? p : lane, up = wave_read(depth, q), next = wave_read(p, q);
+        if (p >= 0) depth += up, p = next;
+    }
+    return 0;
+}
+
+constexpr int kSlots = 16;             // slots of a tile: what a page holds at least, and whole 32 bytes of a row of V
+
+template <typename T>
+struct Piece;                          // 16 bytes of a row
+template <>
+struct Piece<bf16_t> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void widen(const uint4 &v, float (&o)[8]) {
+        o[0] = bf16_lo(v.x), o[1] = bf16_hi(v.x), o[2] = bf16_lo(v.y), o[3] = bf16_hi(v.y);
+        o[4] = bf16_lo(v.z), o[5] = bf16_hi(v.z), o[6] = bf16_lo(v.w), o[7] = bf16_hi(v.w);
+    }
+    static __device__ __forceinline__ uint4 round(const float (&o)[8]) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (bf16_t)o[e];
+        return __builtin_bit_cast(uint4, v);
+    }
+};
+template <>
+struct Piece<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void widen(const uint4 &v, float (&o)[4]) {
+        o[0] = __uint_as_float(v.x), o[1] = __uint_as_float(v.y), o[2] = __uint_as_float(v.z), o[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ uint4 round(const float (&o)[4]) {
+        return make_uint4(__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
+    }
+};
+
+// Tiles of 16 slots as they lie in the cache, so that a row of V of 16 tokens is written whole: workgroup (tile, sequence, up
+// to HC heads of q, of k or of v).  q and k: TL lanes hold a row, 16 bytes each; a team stays with its node, whose cosines and
+// sines it keeps, and all of its rows are requested at once.  Pairs half the rotated columns apart are another lane's 16 bytes.
+// v: turned round in LDS, so that 16 bytes of a column of the tile go out at once.
+template <typename T, int TL, int HC, bool HALF>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv, int zq, int zk) {
+    constexpr int E = Piece<T>::E, TEAMS = kThreads / TL;
+    __shared__ TreeLds tree;
+    __shared__ union { float2 turn[kSlots][128]; T v[kSlots][256 + 2]; } lds;
+    const int b = blockIdx.y, P = kv.dim, tid = threadIdx.x, lane = tid & 63, z = blockIdx.z;
+    const int len = a.lengths[b];
+    int bad = 0;
+    if (len >= 0) {
+        if (!kv.fits((int64_t)len + a.n)) {
+            bad = STREE_SEQ_LENGTH;
+        } else if (a.parent && a.n <= 64) {            // (all waves find the same)
+            int depth = 0;
+            bad = wave_depths(a.parent + (size_t)b * a.n, a.n, lane, depth);
+            tree.cnt[lane] = depth + 1;
+        } else {
+            bad = index_nodes(tree, nullptr, a.parent, b, a.n, 0);
+        }
+        if (bad == 0 && pages_missing(kv, b, len, (int64_t)len + a.n)) bad = STREE_SEQ_PAGE;      // (a barrier)
+    }
+    if (a.status && blockIdx.x == 0 && z == 0 && tid == 0) a.status[b] = bad;
+    const bool dead = len < 0 || bad, query = z < zq, value = z >= zq + zk;
+    if (dead && !query) return;
+    const int slot0 = (dead ? 0 : len & ~(kSlots - 1)) + (int)blockIdx.x * kSlots, node0 = slot0 - (dead ? 0 : len);     // node of slot 0
+    if (node0 >= a.n) return;
+    const int pg = dead ? 0 : kv.page_of(b, slot0);
+    const int h0 = (query ? z : value ? z - zq - zk : z - zq) * HC, heads = min(HC, (query ? a.heads : kv.heads) - h0);
+    const size_t row0 = (size_t)b * a.n;
+    const long sn = query ? a.q_sn : value ? a.v_sn : a.k_sn;
+    const T *const src = static_cast<const T *>(query ? a.q : value ? a.v : a.k);
+    const int c = tid & (TL - 1), pieces = P / E;
+    if (value) {
+        for (int h = 0; h < heads; ++h) {
+            for (int s = tid / TL; s < kSlots; s += TEAMS) {
+                const int i = node0 + s;
+                if (i >= 0 && i < a.n && c < pieces) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (row0 + i) * sn + (size_t)(h0 + h) * P + c * E);
+                    const T *const w = reinterpret_cast<const T *>(&v);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) lds.v[s][c * E + e] = w[e];
+                }
+            }
+            __syncthreads();
+            T *const dst = kv.value(pg, h0 + h, slot0);
+            for (int y = tid; y < P * (kSlots / E); y += kThreads) {
+                const int p = y / (kSlots / E), s = y % (kSlots / E) * E, i = node0 + s;
+                T *const to = dst + ((size_t)p << kv.shift) + s;
+                T w[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] = lds.v[s + e][p];
+                if (i >= 0 && i + E <= a.n) {
+                    uint4 v;
+                    __builtin_memcpy(&v, w, sizeof(v));
+                    *reinterpret_cast<uint4 *>(to) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (i + e >= 0 && i + e < a.n) to[e] = w[e];
+                }
+            }
+            __syncthreads();
+        }
+        return;
+    }
+    T *const out = static_cast<T *>(a.q_out);
+    if (dead) {
+        for (int s = tid / TL; s < kSlots; s += TEAMS)
+            if (node0 + s < a.n && c < pieces)
+                for (int h = 0; h < heads; ++h)
+                    *reinterpret_cast<uint4 *>(out + ((row0 + node0 + s) * a.heads + h0 + h) * P + c * E) = make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
+    const int half = a.rotary / 2, cc = min(c, pieces - 1), col = cc * E;
+    uint4 raw[HC];
+    auto request = [&](int s) {
+        const T *const row = src + (row0 + min(max(node0 + s, 0), a.n - 1)) * sn + col;
+#pragma unroll
+        for (int h = 0; h < HC; ++h) raw[h] = *reinterpret_cast<const uint4 *>(row + (size_t)(h0 + min(h, heads - 1)) * P);
+    };
+    request(tid / TL);
+    for (int y = tid; y < kSlots * half; y += kThreads) {
+        const int s = y / half, j = y - s * half, i = node0 + s;
+        if (i >= 0 && i < a.n) {
+            const int d = a.parent ? tree.cnt[i] - 1 : i;
+            lds.turn[s][j] = rotation(a.turns[j], len + d, a.scale);
+        }
+    }
+    __syncthreads();
+    // of this lane's columns: the weights, and where its pairs' other halves are
+    const bool norm = query ? a.q_norm != nullptr : a.k_norm != nullptr;
+    const T *const w = static_cast<const T *>(query ? a.q_norm : a.k_norm);
+    const int team = lane & ~(TL - 1);
+    const bool second = HALF && col >= half && col < a.rotary, turns = col < a.rotary;
+    const int other = !HALF || !turns ? cc : second ? cc - half / E : cc + half / E;
+    float wo[E], wp[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) wo[e] = wp[e] = 1.f;
+    if (norm) {
+        Piece<T>::widen(*reinterpret_cast<const uint4 *>(w + col), wo);
+        Piece<T>::widen(*reinterpret_cast<const uint4 *>(w + other * E), wp);
+    }
+    for (int s0 = 0; s0 < kSlots; s0 += TEAMS) {
+        const int s = s0 + tid / TL, i = node0 + s;
+        const bool there = s < kSlots && i >= 0 && i < a.n;
+        float cs[E], sn2[E];                           // cosine and sine of each column's pair, the sine with the sign of its place
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            cs[e] = 1.f, sn2[e] = 0.f;
+            const int x = col + e;
+            if (x < a.rotary) {
+                const float2 t = lds.turn[min(s, kSlots - 1)][HALF ? (second ? x - half : x) : x >> 1];
+                const bool up = HALF ? second : (e & 1);
+                cs[e] = t.x, sn2[e] = up ? t.y : -t.y;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < HC; ++h) {
+            if (h >= heads) break;
+            float x[E], y[E], r = 1.f;
+            Piece<T>::widen(raw[h], x);
+            if (norm) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
+                if (c >= pieces) ss = 0.f;
+#pragma unroll
+                for (int o = TL / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
+                r = 1.f / sqrtf(ss / (float)P + a.eps);
+            }
+            if (HALF) {
+                uint4 q;
+                q.x = wave_read(raw[h].x, team + other), q.y = wave_read(raw[h].y, team + other);
+                q.z = wave_read(raw[h].z, team + other), q.w = wave_read(raw[h].w, team + other);
+                Piece<T>::widen(q, y);
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = norm ? y[e] * r * wp[e] : y[e];
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = norm ? x[e] * r * wo[e] : x[e];
+            float z2[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) z2[e] = turns && col + e < a.rotary ? x[e] * cs[e] + (HALF ? y[e] : x[e ^ 1]) * sn2[e] : x[e];
+            if (there && c < pieces)
+                *reinterpret_cast<uint4 *>((query ? out + ((row0 + i) * a.heads + h0 + h) * P : kv.key(pg, h0 + h, slot0 + s)) + col) = Piece<T>::round(z2);
+        }
+        if (s0 + TEAMS < kSlots) request(s + TEAMS);
+    }
+}
+
+template <typename T, int TL, int HC>
+void launch_tuned(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t st) {
+    const int zq = (a.heads + HC - 1) / HC, zk = (kv.nheads_kv + HC - 1) / HC;
+    const dim3 grid((unsigned)((a.n + 2 * kSlots - 2) / kSlots), (unsigned)batch, (unsigned)(zq + 2 * zk));
+    if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, TL, HC, false>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
+    else hipLaunchKernelGGL((rope_kernel<T, TL, HC, true>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
+}
+
 template <typename T>
 hipError_t launch(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t st) {
-    hipLaunchKernelGGL((rope_plain_kernel<T>), dim3((unsigned)(a.n < (1 << 20) ? a.n : 1 << 20), (unsigned)batch), dim3(kThreads), 0, st, a,
-                       KvView<T>(kv));
+    constexpr int E = Piece<T>::E;
+    const int pieces = kv.headdim / E;
+    const bool whole = kv.headdim % E == 0 && a.q_sn % E == 0 && a.k_sn % E == 0 && a.v_sn % E == 0 && (a.interleaved || a.rotary / 2 % E == 0) &&
+                       (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.q_norm | (uintptr_t)a.k_norm |
+                         (uintptr_t)kv.k | (uintptr_t)kv.v) % 16) == 0 && a.heads <= 65535 / 2 && kv.nheads_kv <= 65535 / 4;
+    if (!whole) {
+        hipLaunchKernelGGL((rope_plain_kernel<T>), dim3((unsigned)(a.n < (1 << 20) ? a.n : 1 << 20), (unsigned)batch), dim3(kThreads), 0, st, a,
+                           KvView<T>(kv));
+        return hipGetLastError();
+    }
+    // heads of a workgroup: few where there are few workgroups, so that a step of a few nodes is over sooner
+    const int64_t groups = (int64_t)batch * ((a.n + kSlots - 1) / kSlots) * ((a.heads + 2 * kv.nheads_kv + 7) / 8);
+    const bool few = groups < 128;
+#define STREE_ROPE(TL) (few ? launch_tuned<T, TL, 2>(a, kv, batch, st) : launch_tuned<T, TL, 8>(a, kv, batch, st))
+    if (pieces <= 8) STREE_ROPE(8);
+    else if (pieces <= 16) STREE_ROPE(16);
+    else if (pieces <= 32) STREE_ROPE(32);
+    else STREE_ROPE(64);
+#undef STREE_ROPE
     return hipGetLastError();
 }
 
