@@ -150,9 +150,26 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
     __shared__ union { float2 turn[kSlots][128]; T v[kSlots][256 + 2]; } lds;
     const int b = blockIdx.y, P = kv.dim, tid = threadIdx.x, lane = tid & 63, z = blockIdx.z;
     const int len = a.lengths[b];
+    const bool fits = len >= 0 && kv.fits((int64_t)len + a.n), query = z < zq, value = z >= zq + zk;
+    const int slot0 = (fits ? len & ~(kSlots - 1) : 0) + (int)blockIdx.x * kSlots, node0 = slot0 - (fits ? len : 0);     // node of slot 0
+    if (node0 >= a.n) return;                          // (no first tile does)
+    const int h0 = (query ? z : value ? z - zq - zk : z - zq) * HC, heads = min(HC, (query ? a.heads : kv.heads) - h0);
+    const size_t row0 = (size_t)b * a.n;
+    const long sn = query ? a.q_sn : value ? a.v_sn : a.k_sn;
+    const T *const src = static_cast<const T *>(query ? a.q : value ? a.v : a.k);
+    const int c = tid & (TL - 1), pieces = P / E, cc = min(c, pieces - 1), col = cc * E;
+    // the first rows are on their way while the tree and the pages are looked at
+    uint4 raw[HC];
+    auto request = [&](int s) {
+        const T *const row = src + (row0 + min(max(node0 + s, 0), a.n - 1)) * sn + col;
+#pragma unroll
+        for (int h = 0; h < HC; ++h) raw[h] = *reinterpret_cast<const uint4 *>(row + (size_t)(h0 + min(h, heads - 1)) * P);
+    };
+    request(tid / TL);
+    const int pg = fits ? kv.page_of(b, slot0) : 0;
     int bad = 0;
     if (len >= 0) {
-        if (!kv.fits((int64_t)len + a.n)) {
+        if (!fits) {
             bad = STREE_SEQ_LENGTH;
         } else if (a.parent && a.n <= 64) {            // (all waves find the same)
             int depth = 0;
@@ -164,25 +181,17 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
         if (bad == 0 && pages_missing(kv, b, len, (int64_t)len + a.n)) bad = STREE_SEQ_PAGE;      // (a barrier)
     }
     if (a.status && blockIdx.x == 0 && z == 0 && tid == 0) a.status[b] = bad;
-    const bool dead = len < 0 || bad, query = z < zq, value = z >= zq + zk;
+    const bool dead = len < 0 || bad;
     if (dead && !query) return;
-    const int slot0 = (dead ? 0 : len & ~(kSlots - 1)) + (int)blockIdx.x * kSlots, node0 = slot0 - (dead ? 0 : len);     // node of slot 0
-    if (node0 >= a.n) return;
-    const int pg = dead ? 0 : kv.page_of(b, slot0);
-    const int h0 = (query ? z : value ? z - zq - zk : z - zq) * HC, heads = min(HC, (query ? a.heads : kv.heads) - h0);
-    const size_t row0 = (size_t)b * a.n;
-    const long sn = query ? a.q_sn : value ? a.v_sn : a.k_sn;
-    const T *const src = static_cast<const T *>(query ? a.q : value ? a.v : a.k);
-    const int c = tid & (TL - 1), pieces = P / E;
     if (value) {
         for (int h = 0; h < heads; ++h) {
             for (int s = tid / TL; s < kSlots; s += TEAMS) {
                 const int i = node0 + s;
                 if (i >= 0 && i < a.n && c < pieces) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (row0 + i) * sn + (size_t)(h0 + h) * P + c * E);
+                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (row0 + i) * sn + (size_t)(h0 + h) * P + col);
                     const T *const w = reinterpret_cast<const T *>(&v);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) lds.v[s][c * E + e] = w[e];
+                    for (int e = 0; e < E; ++e) lds.v[s][col + e] = w[e];
                 }
             }
             __syncthreads();
@@ -210,19 +219,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
     T *const out = static_cast<T *>(a.q_out);
     if (dead) {
         for (int s = tid / TL; s < kSlots; s += TEAMS)
-            if (node0 + s < a.n && c < pieces)
+            if (node0 + s >= 0 && node0 + s < a.n && c < pieces)
                 for (int h = 0; h < heads; ++h)
                     *reinterpret_cast<uint4 *>(out + ((row0 + node0 + s) * a.heads + h0 + h) * P + c * E) = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    const int half = a.rotary / 2, cc = min(c, pieces - 1), col = cc * E;
-    uint4 raw[HC];
-    auto request = [&](int s) {
-        const T *const row = src + (row0 + min(max(node0 + s, 0), a.n - 1)) * sn + col;
-#pragma unroll
-        for (int h = 0; h < HC; ++h) raw[h] = *reinterpret_cast<const uint4 *>(row + (size_t)(h0 + min(h, heads - 1)) * P);
-    };
-    request(tid / TL);
+    const int half = a.rotary / 2;
     for (int y = tid; y < kSlots * half; y += kThreads) {
         const int s = y / half, j = y - s * half, i = node0 + s;
         if (i >= 0 && i < a.n) {
@@ -247,15 +249,16 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
     for (int s0 = 0; s0 < kSlots; s0 += TEAMS) {
         const int s = s0 + tid / TL, i = node0 + s;
         const bool there = s < kSlots && i >= 0 && i < a.n;
-        float cs[E], sn2[E];                           // cosine and sine of each column's pair, the sine with the sign of its place
+        // y = r (A x + B x'), x' the pair's other half: weights, cosine and sine (its sign that of the place) of each column
+        float A[E], B[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            cs[e] = 1.f, sn2[e] = 0.f;
+            A[e] = wo[e], B[e] = 0.f;
             const int x = col + e;
             if (x < a.rotary) {
                 const float2 t = lds.turn[min(s, kSlots - 1)][HALF ? (second ? x - half : x) : x >> 1];
-                const bool up = HALF ? second : (e & 1);
-                cs[e] = t.x, sn2[e] = up ? t.y : -t.y;
+                A[e] = wo[e] * t.x;
+                B[e] = (HALF ? wp[e] : wo[e ^ 1]) * ((HALF ? second : (e & 1)) ? t.y : -t.y);
             }
         }
 #pragma unroll
@@ -277,16 +280,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
                 q.x = wave_read(raw[h].x, team + other), q.y = wave_read(raw[h].y, team + other);
                 q.z = wave_read(raw[h].z, team + other), q.w = wave_read(raw[h].w, team + other);
                 Piece<T>::widen(q, y);
-#pragma unroll
-                for (int e = 0; e < E; ++e) y[e] = norm ? y[e] * r * wp[e] : y[e];
             }
+            float out8[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = norm ? x[e] * r * wo[e] : x[e];
-            float z2[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) z2[e] = turns && col + e < a.rotary ? x[e] * cs[e] + (HALF ? y[e] : x[e ^ 1]) * sn2[e] : x[e];
+            for (int e = 0; e < E; ++e) {
+                const float turned = fmaf(HALF ? y[e] : x[e ^ 1], B[e], x[e] * A[e]);
+                out8[e] = r * (col + e < a.rotary ? turned : x[e] * A[e]);
+            }
             if (there && c < pieces)
-                *reinterpret_cast<uint4 *>((query ? out + ((row0 + i) * a.heads + h0 + h) * P : kv.key(pg, h0 + h, slot0 + s)) + col) = Piece<T>::round(z2);
+                *reinterpret_cast<uint4 *>((query ? out + ((row0 + i) * a.heads + h0 + h) * P : kv.key(pg, h0 + h, slot0 + s)) + col) = Piece<T>::round(out8);
         }
         if (s0 + TEAMS < kSlots) request(s + TEAMS);
     }
@@ -312,10 +314,14 @@ hipError_t launch(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t 
                            KvView<T>(kv));
         return hipGetLastError();
     }
-    // heads of a workgroup: few where there are few workgroups, so that a step of a few nodes is over sooner
+    // Heads of a workgroup: two where there are few workgroups, so that a step of a few nodes is over sooner; eight bf16 heads,
+    // which share their node's angles, where there are many (four prompts of 2048 tokens 55 us, with four heads 58); else four
+    // (16 trees of 64 nodes 13.8 us, with eight 14.4; two fp32 prompts of 2047 tokens 39 and 43 us).
     const int64_t groups = (int64_t)batch * ((a.n + kSlots - 1) / kSlots) * ((a.heads + 2 * kv.nheads_kv + 7) / 8);
-    const bool few = groups < 128;
-#define STREE_ROPE(TL) (few ? launch_tuned<T, TL, 2>(a, kv, batch, st) : launch_tuned<T, TL, 8>(a, kv, batch, st))
+    constexpr int kMany = E == 8 ? 8 : 4;
+#define STREE_ROPE(TL)                                                        \
+    (groups < 128 ? launch_tuned<T, TL, 2>(a, kv, batch, st)                  \
+                  : groups < 2048 ? launch_tuned<T, TL, 4>(a, kv, batch, st) : launch_tuned<T, TL, kMany>(a, kv, batch, st))
     if (pieces <= 8) STREE_ROPE(8);
     else if (pieces <= 16) STREE_ROPE(16);
     else if (pieces <= 32) STREE_ROPE(32);
