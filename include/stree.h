@@ -373,7 +373,7 @@ typedef struct stree_kv {
     int32_t npages;    /* pages of the pool, >= 1 */
     int32_t page;      /* tokens a page: 16, 32, 64, 128 or 256 */
     int32_t max_pages; /* entries of a row of `table`, >= 1; max_pages * page <= 2^30 */
-    int32_t nheads_kv; /* >= 1 */
+    int32_t nheads_kv; /* >= 1; nlayers * nheads_kv <= 2^23, nheads_kv * headdim * page <= 2^28 */
     int32_t headdim;   /* 1..256 */
     int32_t io_dtype;  /* enum stree_dtype: the cache, queries, outputs */
     int32_t reserved;  /* 0 */

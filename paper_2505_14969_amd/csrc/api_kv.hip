@@ -17,6 +17,7 @@ int check_kv(const stree_kv *kv, bool one_layer) {
     if (kv->page < 16 || kv->page > 256 || (kv->page & (kv->page - 1))) return STREE_ERR_BAD_SHAPE;
     if ((int64_t)kv->max_pages * kv->page > (1LL << 30)) return STREE_ERR_BAD_SHAPE;
     if (kv->nheads_kv < 1 || kv->nheads_kv > 65535 || kv->headdim < 1 || kv->headdim > 256) return STREE_ERR_BAD_SHAPE;
+    if ((int64_t)kv->nlayers * kv->nheads_kv > (1 << 23)) return STREE_ERR_BAD_SHAPE;      // (a grid dimension)
     // (a page of all heads is moved with 32-bit offsets)
     if ((int64_t)kv->nheads_kv * kv->headdim * kv->page > (1LL << 28)) return STREE_ERR_BAD_SHAPE;
     return STREE_OK;

@@ -1,7 +1,11 @@
 // stree_commit_kv: the rows of the accepted path, root first, moved together behind the text, in every layer, and the new lengths.
 //   [len + t] <- [len + p_t], t = 0 .. d
 // p_t >= t and p grows with t, so a row that is still to be read never lies where an earlier one was put: each thread moves its
-// own columns in the order of t, in place.
+// own columns in the order of t, a few rows at once, in place.
+//
+// A few rows of a few hundred bytes in each of many places: bound by the chain length -> tree -> page numbers -> rows, and by
+// how many places are worked on at once.  So a workgroup takes up to kHeads heads of a layer behind one look at the tree, where
+// there are enough workgroups, and page numbers are looked up for all rows at once.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 
@@ -15,69 +19,131 @@ struct CommitArgs {
     int n;
 };
 
-// Workgroup (layer x head, sequence); MOVE false: lengths and status only, one workgroup per sequence.
-template <typename T, bool MOVE>
-__global__ __launch_bounds__(kThreads) void commit_kv_kernel(CommitArgs a, KvView<T> kv, size_t layer_elems) {
+constexpr int kBatch = 8;              // rows that a thread has on their way
+
+// The accepted path of sequence b: its nodes, root first, in `path`, and how many (0: nothing to move), or what is wrong.  Up
+// to 64 nodes every wave follows the parents in its own lanes.
+template <typename T>
+__device__ __forceinline__ int find_path(const CommitArgs &a, const KvView<T> &kv, TreeLds &tree, uint32_t *bits, int *path, int b, int len,
+                                         int k, int &count) {
+    count = 0;
+    if (len < 0) return 0;
+    if (!kv.fits((int64_t)len + a.n)) return STREE_SEQ_LENGTH;
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (a.parent && a.n <= 64) {
+        const int p = lane < a.n ? a.parent[(size_t)b * a.n + lane] : -1;
+        const unsigned long long wrong = __ballot(lane < a.n && (lane == 0 ? p != -1 : (p < 0 || p >= lane)));
+        if (wrong) return __ffsll((long long)wrong);
+        if (k < -1 || k >= a.n) return STREE_SEQ_ACCEPTED;
+        unsigned long long on = 0;
+        for (int j = __builtin_amdgcn_readfirstlane(k); j >= 0; j = __builtin_amdgcn_readlane(p, j)) on |= 1ull << j;      // (p < j)
+        count = __popcll(on);
+        if ((on >> lane) & 1ull) path[__popcll(on & ((1ull << lane) - 1ull))] = lane;
+    } else {
+        const int words = (a.n + 31) / 32;
+        if (const int node = index_nodes(tree, bits, a.parent, b, a.n, words)) return node;
+        if (k < -1 || k >= a.n) return STREE_SEQ_ACCEPTED;
+        if (k >= 0) count = a.parent ? tree.cnt[k] : k + 1;
+        if (a.parent && k >= 0 && tid <= k && tid < kMaxNodes && mask_bit(bits, words, k, tid)) {
+            int t = 0;
+            for (int w = 0; w < words; ++w)
+                t += __popc(bits[k * words + w] & (w < (tid >> 5) ? ~0u : w == (tid >> 5) ? (1u << (tid & 31)) - 1u : 0u));
+            path[t] = tid;
+        }
+    }
+    if (k >= 0 && pages_missing(kv, b, len, (int64_t)len + k + 1)) {          // (a barrier: `path` is there)
+        count = 0;
+        return STREE_SEQ_PAGE;
+    }
+    return 0;
+}
+
+// Workgroup (heads of a layer, sequence); MOVE false: lengths and status only, one workgroup per sequence.  E: elements of K
+// moved at once.
+template <typename T, bool MOVE, int E>
+__global__ __launch_bounds__(kThreads) void commit_kv_kernel(CommitArgs a, KvView<T> kv, size_t layer_elems, int chunks, int per) {
+    typedef T Run __attribute__((ext_vector_type(E)));
     __shared__ TreeLds tree;
     __shared__ uint32_t bits[kMaxNodes * kMaxWords];
     __shared__ int path[kMaxNodes];
-    const int b = blockIdx.y, tid = threadIdx.x;
-    const int len = a.lengths[b], k = a.accepted[b], words = (a.n + 31) / 32;
-    int bad = 0, count = 0;
-    if (len >= 0) {
-        if (!kv.fits((int64_t)len + a.n)) {
-            bad = STREE_SEQ_LENGTH;
-        } else if (int node = index_nodes(tree, bits, a.parent, b, a.n, words)) {
-            bad = node;
-        } else if (k < -1 || k >= a.n) {
-            bad = STREE_SEQ_ACCEPTED;
-        } else if (k >= 0) {
-            count = a.parent ? tree.cnt[k] : k + 1;
-            if (pages_missing(kv, b, len, (int64_t)len + k + 1)) bad = STREE_SEQ_PAGE, count = 0;
-        }
-    }
+    __shared__ int2 from[kMaxNodes], to[kMaxNodes];              // (page, token within it)
+    const int b = blockIdx.y, tid = threadIdx.x, len = a.lengths[b], k = a.accepted[b];
+    int count;
+    const int bad = find_path(a, kv, tree, bits, path, b, len, k, count);
     if (blockIdx.x == 0 && tid == 0) {
         if (a.lengths_out) a.lengths_out[b] = len + count;
         if (a.status) a.status[b] = bad;
     }
     if (!MOVE || count == 0 || !a.parent) return;
-    if (tid <= k && mask_bit(bits, words, k, tid)) {
-        int t = 0;
-        for (int w = 0; w < words; ++w)
-            t += __popc(bits[k * words + w] & (w < (tid >> 5) ? ~0u : w == (tid >> 5) ? (1u << (tid & 31)) - 1u : 0u));
-        path[t] = tid;
+    if (tid < count) {
+        const int s = len + path[tid], d = len + tid;
+        from[tid] = make_int2(kv.page_of(b, s), s & kv.mask());
+        to[tid] = make_int2(kv.page_of(b, d), d & kv.mask());
     }
+    int first = 0;                                               // (the first rows mostly stand where they should)
+    while (first < count && path[first] == first) ++first;
     __syncthreads();
-    const int layer = blockIdx.x / kv.heads, g = blockIdx.x % kv.heads;
-    kv.k += layer * layer_elems;
-    kv.v += layer * layer_elems;
-    for (int e = tid; e < kv.dim; e += kThreads)
-        for (int t = 0; t < count; ++t) {
-            const int from = len + path[t], to = len + t;
-            if (from == to) continue;
-            const int pf = kv.page_of(b, from), pt = kv.page_of(b, to);
-            kv.key(pt, g, to)[e] = kv.key(pf, g, from)[e];
-            kv.value(pt, g, to)[(size_t)e << kv.shift] = kv.value(pf, g, from)[(size_t)e << kv.shift];
+    const int layer = blockIdx.x / chunks, g0 = blockIdx.x % chunks * per, heads = min(per, kv.heads - g0);
+    T *const kl = kv.k + layer * layer_elems, *const vl = kv.v + layer * layer_elems;
+    const int runs = kv.dim / E, keys = heads * runs, all = keys + heads * kv.dim;
+    const size_t block = (size_t)kv.dim << kv.shift;
+    for (int y = tid; y < all; y += kThreads) {
+        if (y < keys) {
+            const int g = g0 + y / runs, c = y % runs * E;
+            auto at = [&](const int2 &w) { return reinterpret_cast<Run *>(kl + ((size_t)w.x * kv.heads + g) * block + (size_t)w.y * kv.dim + c); };
+            for (int t = first; t < count; t += kBatch) {
+                Run r[kBatch];
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x) r[x] = *at(from[min(t + x, count - 1)]);
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x)
+                    if (t + x < count) *at(to[t + x]) = r[x];
+            }
+        } else {
+            const int g = g0 + (y - keys) / kv.dim;
+            const size_t p = (size_t)((y - keys) % kv.dim) << kv.shift;
+            auto at = [&](const int2 &w) { return vl + ((size_t)w.x * kv.heads + g) * block + p + w.y; };
+            for (int t = first; t < count; t += kBatch) {
+                T r[kBatch];
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x) r[x] = *at(from[min(t + x, count - 1)]);
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x)
+                    if (t + x < count) *at(to[t + x]) = r[x];
+            }
         }
+    }
 }
 
-template <typename T>
-hipError_t launch(CommitArgs a, const stree_kv &kv, int batch, hipStream_t st) {
+template <typename T, int E>
+hipError_t launch_runs(CommitArgs a, const stree_kv &kv, int batch, hipStream_t st) {
     const KvView<T> view(kv);
     const size_t layer = (size_t)kv.npages * kv.nheads_kv * kv.page * kv.headdim;
+    // Heads of a workgroup: one until there are as many workgroups as the chip holds at once, then more.
+    const int64_t places = (int64_t)batch * kv.nlayers * kv.nheads_kv;
+    int per = (int)((places + 2047) / 2048);
+    per = per < kv.nheads_kv ? per : kv.nheads_kv;
+    const int chunks = (kv.nheads_kv + per - 1) / per;
     // A chain's rows stand where they should.  Lengths that are overwritten are so when every workgroup has read them.
     const CommitArgs after = a;
     const bool apart = !a.parent || a.lengths == a.lengths_out;
     if (a.parent) {
         if (apart) a.lengths_out = a.status = nullptr;
-        hipLaunchKernelGGL((commit_kv_kernel<T, true>), dim3((unsigned)kv.nlayers * kv.nheads_kv, (unsigned)batch), dim3(kThreads), 0, st, a,
-                           view, layer);
+        hipLaunchKernelGGL((commit_kv_kernel<T, true, E>), dim3((unsigned)kv.nlayers * chunks, (unsigned)batch), dim3(kThreads), 0, st, a, view,
+                           layer, chunks, per);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (apart)
-        hipLaunchKernelGGL((commit_kv_kernel<T, false>), dim3(1, (unsigned)batch), dim3(kThreads), 0, st, after, view, layer);
+        hipLaunchKernelGGL((commit_kv_kernel<T, false, E>), dim3(1, (unsigned)batch), dim3(kThreads), 0, st, after, view, layer, chunks, per);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch(const CommitArgs &a, const stree_kv &kv, int batch, hipStream_t st) {
+    constexpr int E = 16 / sizeof(T);
+    if (kv.headdim % E == 0 && (uintptr_t)kv.k % 16 == 0) return launch_runs<T, E>(a, kv, batch, st);
+    return launch_runs<T, 1>(a, kv, batch, st);
 }
 
 }  // namespace
