@@ -101,72 +101,87 @@ __global__ __launch_bounds__(kPool) void resize_kernel(PoolView p, int batch, co
     }
     __syncthreads();
     const int drops = scan_rows(first, batch, part);
-    for (int x = tid; x < drops; x += kPool) {
-        const int b = row_of(first, batch, x), pg = p.row(b)[need[b] + x - first[b]];
-        if (p.exists(pg)) atomicSub(&p.refs[pg], 1);
-    }
-    __syncthreads();
-    // the first entry of a page that nobody holds any more claims it
-    for (int x = tid; x < drops; x += kPool) {
-        const int b = row_of(first, batch, x), pg = p.row(b)[need[b] + x - first[b]];
-        if (!p.exists(pg)) {
-            state[b] = STREE_SEQ_PAGE;
-            continue;
+    if (drops) {                                       // (alike in all threads)
+        // An entry's row and page: a thread's first entry is looked up once.
+        struct Entry { int b, j, pg; };
+        auto entry = [&](int x) {
+            Entry e;
+            e.b = row_of(first, batch, x), e.j = need[e.b] + x - first[e.b], e.pg = p.row(e.b)[e.j];
+            return e;
+        };
+        Entry mine = {0, 0, -1};
+        if (tid < drops) mine = entry(tid);
+        auto at = [&](int x) { return x == tid ? mine : entry(x); };
+        for (int x = tid; x < drops; x += kPool) {
+            const int pg = at(x).pg;
+            if (p.exists(pg)) atomicSub(&p.refs[pg], 1);
         }
-        const int r = load_count(&p.refs[pg]);
-        if (r == 0 || r < kClaim / 2) atomicMin(&p.refs[pg], kClaim + x);
-        else if (r < 0) state[b] = STREE_SEQ_PAGE;                    // (dropped more often than held)
-    }
-    __syncthreads();
-    for (int x0 = 0; x0 < drops; x0 += kPool) {
-        const int x = x0 + tid;
-        int pg = -1;
-        if (x < drops) {
-            const int b = row_of(first, batch, x), e = p.row(b)[need[b] + x - first[b]];
-            if (p.exists(e) && load_count(&p.refs[e]) == kClaim + x) pg = e;
+        __syncthreads();
+        // the first entry of a page that nobody holds any more claims it
+        for (int x = tid; x < drops; x += kPool) {
+            const Entry e = at(x);
+            if (!p.exists(e.pg)) {
+                state[e.b] = STREE_SEQ_PAGE;
+                continue;
+            }
+            const int r = load_count(&p.refs[e.pg]);
+            if (r == 0 || r < kClaim / 2) atomicMin(&p.refs[e.pg], kClaim + x);
+            else if (r < 0) state[e.b] = STREE_SEQ_PAGE;              // (dropped more often than held)
         }
-        int all;
-        const int at = nf + block_scan(pg >= 0, part, all);
-        if (pg >= 0 && at < p.npages) p.free[at] = pg;
-        nf = min(nf + all, p.npages);
+        __syncthreads();
+        int held_on = 1;                               // what refs says of a thread's first page: other than negative, nothing is to be done
+        for (int x0 = 0; x0 < drops; x0 += kPool) {
+            const int x = x0 + tid;
+            int pg = -1;
+            if (x < drops) {
+                const Entry e = at(x);
+                const int r = p.exists(e.pg) ? load_count(&p.refs[e.pg]) : 1;
+                if (x0 == 0) held_on = r;
+                if (r == kClaim + x) pg = e.pg;
+            }
+            int all;
+            const int to = nf + block_scan(pg >= 0, part, all);
+            if (pg >= 0 && to < p.npages) p.free[to] = pg;
+            nf = min(nf + all, p.npages);
+        }
+        __syncthreads();
+        for (int x = tid; x < drops; x += kPool) {
+            const Entry e = at(x);
+            if (p.exists(e.pg) && (x == tid ? held_on : load_count(&p.refs[e.pg])) < 0) store_count(&p.refs[e.pg], 0);
+            p.row(e.b)[e.j] = -1;
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int x = tid; x < drops; x += kPool) {
-        const int b = row_of(first, batch, x), j = need[b] + x - first[b], pg = p.row(b)[j];
-        if (p.exists(pg) && load_count(&p.refs[pg]) < 0) store_count(&p.refs[pg], 0);
-        p.row(b)[j] = -1;
-    }
-    __syncthreads();
     // growth: a prefix of the growing rows, as far as the free pages go
     for (int b = tid; b < batch; b += kPool) {
         const int h = p.held[b];
         first[b] = need[b] > h ? need[b] - h : 0;
     }
     __syncthreads();
-    scan_rows(first, batch, part);
     int taken = 0;
-    for (int b0 = 0; b0 < batch; b0 += kPool) {
-        const int b = b0 + tid;
-        int grow = 0;
-        if (b < batch) {
-            grow = first[b + 1] - first[b];
-            if (grow && first[b + 1] > nf) {
-                state[b] = STREE_SEQ_POOL;
-                grow = 0;
+    if (scan_rows(first, batch, part)) {
+        for (int b0 = 0; b0 < batch; b0 += kPool) {
+            const int b = b0 + tid;
+            int grow = 0;
+            if (b < batch) {
+                grow = first[b + 1] - first[b];
+                if (grow && first[b + 1] > nf) {
+                    state[b] = STREE_SEQ_POOL;
+                    grow = 0;
+                }
             }
+            int all;
+            block_scan(grow, part, all);
+            taken += all;
         }
-        int all;
-        block_scan(grow, part, all);
-        taken += all;
+        for (int x = tid; x < taken; x += kPool) {
+            const int b = row_of(first, batch, x), pg = p.free[nf - 1 - x];
+            p.row(b)[need[b] - first[b + 1] + x] = pg;                // (the row's own entries end at need - growth)
+            if (p.exists(pg)) store_count(&p.refs[pg], 1);
+            else state[b] = STREE_SEQ_PAGE;                           // (the stack of free pages is damaged)
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int x = tid; x < taken; x += kPool) {
-        const int b = row_of(first, batch, x), pg = p.free[nf - 1 - x];
-        p.row(b)[p.held[b] + x - first[b]] = pg;
-        if (p.exists(pg)) store_count(&p.refs[pg], 1);
-        else state[b] = STREE_SEQ_PAGE;                               // (the stack of free pages is damaged)
-    }
-    __syncthreads();
     for (int b = tid; b < batch; b += kPool) {
         if (state[b] != STREE_SEQ_POOL) p.held[b] = need[b];
         if (status) status[b] = state[b];
