@@ -468,15 +468,15 @@ struct Shape {
     Shape(const stree_attn &a, const stree_kv &kv) {
         const int rows = a.nnodes * (a.nheads / kv.nheads_kv);
         const int64_t units = (int64_t)a.batch * kv.nheads_kv, most = units * (((int64_t)kv.max_pages * kv.page + kTileKeys - 1) / kTileKeys);
-        shared = kv.io_dtype == STREE_BF16 && (kv.headdim == 64 || kv.headdim == 128) && rows > 64;
+        shared = kv.io_dtype == STREE_BF16 && (kv.headdim == 64 || kv.headdim == 128) && rows > 32;
         if (shared) {
-            blocks = rows <= 128 ? 8 : 16;
+            blocks = rows <= 64 ? 4 : 16;
             tiles = (rows + 16 * blocks - 1) / (16 * blocks);
-            const int w = kChip / tiles < 1 ? 1 : kChip / tiles;
+            const int chip = blocks == 4 ? 2 * kChip : kChip, w = chip / tiles < 1 ? 1 : chip / tiles;
             workers = (int)(w < most ? w : most);
             return;
         }
-        blocks = rows <= 16 ? 1 : rows <= 32 || kv.headdim > 128 ? 2 : 4;
+        blocks = rows <= 16 ? 1 : 2;
         while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
         tiles = (rows + 16 * blocks - 1) / (16 * blocks);
         const int regs = blocks * (kv.headdim <= 64 ? 64 : kv.headdim <= 128 ? 128 : 256);       // (as in StreamShape)
@@ -520,8 +520,7 @@ void launch_stream(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, 
 template <typename T, int PP>
 void launch_rows(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, int blocks, hipStream_t st) {
     if (blocks == 1) launch_stream<T, PP, 1>(a, kv, sp, st);
-    else if (blocks == 2 || PP > 128) launch_stream<T, PP, 2>(a, kv, sp, st);
-    else launch_stream<T, PP, (PP > 128 ? 2 : 4)>(a, kv, sp, st);
+    else launch_stream<T, PP, 2>(a, kv, sp, st);
 }
 
 template <typename T>

@@ -6,8 +6,8 @@
 // of 32 rows each.  (64 rows a wave would halve the operands read from LDS, which need as long as the products; but with 256
 // values in accumulators the compiler spills what is on its way from memory: 16 trees of 64 nodes 199 us where this takes 84.)  As in the streaming kernel a lane owns a query row in every
 // accumulator (S^T = K Q^T, O^T += V^T P^T), keys stand in S^T in the order that makes the probabilities the operand of the
-// second product, and the maximum moves only when a score passes it by kSlack.  Tiles go through registers into two LDS
-// buffers, the next one's loads in flight behind the products: one barrier a tile.
+// second product, and the maximum moves only when a score passes it by kSlack.  Tiles go from memory straight into LDS, the
+// next one or two on their way behind the products: one barrier a tile.
 #include "attn.hpp"
 
 namespace stree {
@@ -16,23 +16,28 @@ namespace {
 
 constexpr float kSlack = 8.f;
 constexpr int kKeys = 64;                            // keys of a tile
-constexpr int kTileThreads = 512;
 
 // Rows of K are 16-byte pieces, permuted by the key, so that eight lanes that read the same piece of keys that follow one
 // another in S^T use all banks; 16 tokens of V are rows of 32 bytes, whose halves change places every four rows.
-template <int PP, int RW>
+template <int PP, int NB>
 struct TileLds {
     static constexpr int kTile = kKeys * PP;         // elements
-    bf16_t k[2][kTile], v[2][kTile];
+    bf16_t t[NB][2][kTile];                          // keys, values
     uint32_t bits[kMaxNodes * kMaxWords];
 };
 
-template <int PP, int RW>
-__global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, KvView<bf16_t> kv, AttnSplit sp) {
-    constexpr int ROWS = 32 * RW, KW = 8 / RW, KB = 2 / KW, NC = PP / 16, NPB = PP / 32;    // key waves; blocks of 32 keys a wave
-    constexpr int PIECES = kKeys * PP / 8 / kTileThreads;                                     // 16-byte pieces of a tile per thread
+// 64 lanes' 16 bytes from memory to LDS, one lane's after the other's from `to` on (alike in all lanes).
+__device__ __forceinline__ void load_to_lds(const bf16_t *from, bf16_t *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// RW waves side by side over the rows, TH / 64 / RW over a tile's keys; NB tiles in LDS, NB - 1 of them on their way.
+template <int PP, int RW, int TH, int NB>
+__global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf16_t> kv, AttnSplit sp) {
+    constexpr int WAVES = TH / 64, ROWS = 32 * RW, KW = WAVES / RW, KB = 2 / KW, NC = PP / 16, NPB = PP / 32;    // key waves; blocks of 32 keys a wave
+    constexpr int LOADS = kKeys * PP / 512 / WAVES;                                   // a wave's loads of 1 KB for a tile's keys, and for its values
     static_assert(KW * KB == 2, "64 keys a tile");
-    typedef TileLds<PP, RW> Lds;
+    typedef TileLds<PP, NB> Lds;
     __shared__ Lds lds;
     __shared__ float ml[KW > 1 ? ROWS : 1][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wr = wave % RW, wk = wave / RW;
@@ -42,19 +47,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
     const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, words = (a.n + 31) / 32;
     bf16_t *const out = static_cast<bf16_t *>(a.out);
     const float scale = fabsf(a.scale);
-    Share at = Share::start<kTileThreads>(a, kv, sp, worker, reinterpret_cast<int64_t *>(lds.k[0]));
+    Share at = Share::start<TH>(a, kv, sp, worker, reinterpret_cast<int64_t *>(lds.t[0]));
     if (worker >= at.workers) return;
     __syncthreads();                                   // (its numbers lay where the first tile goes)
 
-    // where a thread's pieces of a tile lie: K by rows, V by runs of 16 tokens
     const int shift = kv.shift, mask = kv.mask();
     const size_t block = (size_t)PP << shift;
-    constexpr int KR = PP / 8, KSTEP = kTileThreads / KR;                 // pieces of a row of K; rows a pass
-    const int krow = tid / KR, kpiece = tid % KR;
-    constexpr int VP = 2 * PP, VSTEP = kTileThreads / VP;    // pieces of 16 tokens of V; such runs a pass
-    const int vrun = tid / VP, vrow = tid % VP >> 1, vhalf = tid & 1;
-    const int kput = krow * PP + ((kpiece ^ ((krow & 3) | ((krow >> 1) & 4))) * 8);
-    const int vput = vrun * 16 * PP + vrow * 16 + ((vhalf ^ ((vrow >> 2) & 1)) * 8);
+    bf16_t *const scratch = lds.t[NB - 1][0];          // (no tile of a new piece is on its way to the last buffer)
     // where a lane's operands lie
     const int ktok = (col & 3) | ((col >> 1) & 4) | ((col << 1) & 8) | (col & 16);      // S^T row -> key
     // (row r = 4 h + e of a block of 16 holds key 8 h + e, row 8 + 4 h + e key 8 h + 4 + e)
@@ -67,15 +66,20 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
     int k0 = 0, k1 = 0, whole = 0, end = 0;
     PageWalk<bf16_t> walk;
     bf16x8 q[NC];
-    bf16x8 sk[PIECES], sv[PIECES];
-    auto fetch = [&](int t) {                          // a tile's pieces on their way
+    // A tile on its way to a buffer: K by rows of 16-byte pieces, V by runs of 16 tokens, 32 rows of it a load.  What lies where is
+    // a matter of which lane fetches what.
+    auto fetch = [&](int t, int buf) {
         walk.reach(kv, at.b, t >> shift, end, lane);
+        constexpr int KR = PP / 8, VR = PP / 32;       // pieces of a row of K; loads of a run of V
 #pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            const int tk = t + ((x * KSTEP + krow) & ~15), pk = walk.at(uniform(min(tk >> shift, end - 1)));
-            sk[x] = *reinterpret_cast<const bf16x8 *>(kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + x * KSTEP + krow) & mask) * PP + kpiece * 8);
-            const int tv = t + 16 * (x * VSTEP + vrun), pv = walk.at(uniform(min(tv >> shift, end - 1)));
-            sv[x] = *reinterpret_cast<const bf16x8 *>(kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)vrow << shift) + (tv & mask) + vhalf * 8);
+        for (int x = 0; x < LOADS; ++x) {
+            const int y = x * WAVES + wave;
+            const int r = y * (64 / KR) + lane / KR, piece = (lane % KR) ^ ((r & 3) | ((r >> 1) & 4));
+            const int tk = t + ((y * (64 / KR)) & ~15), pk = walk.at(min(tk >> shift, end - 1));
+            load_to_lds(kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + r) & mask) * PP + piece * 8, &lds.t[buf][0][y * 512]);
+            const int run = y / VR, p = (y % VR) * 32 + (lane >> 1), vhalf = (lane & 1) ^ ((p >> 2) & 1);
+            const int tv = t + 16 * run, pv = walk.at(min(tv >> shift, end - 1));
+            load_to_lds(kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)p << shift) + (tv & mask) + vhalf * 8, &lds.t[buf][1][y * 512]);
         }
     };
     auto enter = [&]() {
@@ -96,7 +100,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
 #pragma unroll
             for (int c = 0; c < NC; ++c) q[c] = signed_query(*reinterpret_cast<const bf16x8 *>(src + c * 16), a.scale);
         }
-        fetch(k0);
+#pragma unroll
+        for (int x = 0; x < NB - 1; ++x)
+            if (k0 + x * kKeys < k1) fetch(k0 + x * kKeys, x);
     };
     enter();
     for (;;) {
@@ -106,8 +112,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
         if (whole > len && len >= 0 && whole > 0 && a.parent) {
-            __syncthreads();                           // (the index borrows a tile's place)
-            bad = index_nodes(*reinterpret_cast<TreeLds *>(lds.v[0]), lds.bits, a.parent, b, a.n, words);
+            bad = index_nodes(*reinterpret_cast<TreeLds *>(scratch), lds.bits, a.parent, b, a.n, words);
             __syncthreads();
         }
         const int col = again(lane) & 31, half = again(lane) >> 5;
@@ -123,33 +128,31 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
                 for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
         }
         int buf = 0;
-        for (int t = k0; t < w1; t += kKeys, buf ^= 1) {
+        for (int t = k0; t < w1; t += kKeys, buf = buf == NB - 1 ? 0 : buf + 1) {
             const bool tail = t + kKeys > len || t + kKeys > w1;
-            // Values behind the last node are no numbers anybody wrote.
+            // This wave's part of the tile is there (younger loads, those of the next tile, may be on their way), and with the
+            // barrier everybody's; everybody is done with the tile before this one, whose place the next to be fetched takes.
+            if (NB > 2 && t + kKeys < w1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            if (t + (NB - 1) * kKeys < w1) fetch(t + (NB - 1) * kKeys, buf == 0 ? NB - 1 : buf - 1);
             int odd = 0;
-            if (tail) {
-#pragma unroll
-                for (int x = 0; x < PIECES; ++x) {
-                    const int left = len + a.n - (t + 16 * (x * VSTEP + vrun) + vhalf * 8);
-                    bf16x8 f = sv[x];
+            if (__builtin_expect(tail, 0)) {
+                // Values behind the last node are no numbers anybody wrote.
+                for (int y = tid; y < kKeys * PP / 8; y += TH) {
+                    bf16x8 *const at8 = reinterpret_cast<bf16x8 *>(lds.t[buf][1]) + y;
+                    const int run = y / (2 * PP), p = y % (2 * PP) >> 1, left = len + a.n - (t + 16 * run + ((y ^ (p >> 2)) & 1) * 8);
+                    bf16x8 f = *at8;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         if (e >= left) f[e] = (bf16_t)0.f;
                         odd |= !(fabsf((float)f[e]) < INFINITY);
                     }
-                    sv[x] = f;
+                    *at8 = f;
                 }
+                odd = __syncthreads_or(odd);
             }
-#pragma unroll
-            for (int x = 0; x < PIECES; ++x) {
-                *reinterpret_cast<bf16x8 *>(&lds.k[buf][kput + x * KSTEP * PP]) = sk[x];
-                *reinterpret_cast<bf16x8 *>(&lds.v[buf][vput + x * VSTEP * 16 * PP]) = sv[x];
-            }
-            if (tail) odd = __syncthreads_or(odd);
-            else __syncthreads();
-            if (t + kKeys < w1) fetch(t + kKeys);
 
-            const bf16_t *const kt = lds.k[buf] + wk * 32 * PP, *const vt = lds.v[buf] + wk * 32 * PP;
+            const bf16_t *const kt = lds.t[buf][0] + wk * 32 * PP, *const vt = lds.t[buf][1] + wk * 32 * PP;
             uint32_t seen[KB];                      // 16 keys a block and lane: bits 0 - 7 of its first 16, 8 - 15 of its last
             if (__builtin_expect(tail, 0)) {
 #pragma unroll
@@ -197,8 +200,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
                         }
                     }
                     __syncthreads();
-                    for (int x = tid; x < kKeys * PP; x += kTileThreads)
-                        if (!(fabsf((float)lds.v[buf][x]) < INFINITY)) lds.v[buf][x] = (bf16_t)0.f;
+                    for (int x = tid; x < kKeys * PP; x += TH)
+                        if (!(fabsf((float)lds.t[buf][1][x]) < INFINITY)) lds.t[buf][1][x] = (bf16_t)0.f;
                     __syncthreads();
                 }
             }
@@ -253,7 +256,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
         }
         // (pages of the piece that only later rows see)
         int missing = walk.bad;
-        for (int j = (k1 >> shift) + tid; j < (whole + mask) >> shift; j += kTileThreads) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
+        for (int j = (k1 >> shift) + tid; j < (whole + mask) >> shift; j += TH) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
         if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
         const bool more = at.next(a, kv);
         if (more) enter();                             // the next piece's first tile is on its way
@@ -265,8 +268,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
         l += __shfl_xor(l, 32);
         if constexpr (KW > 1) {
             // the second half of the keys is handed to the first's waves, 32 rows at a time: [wave][p][row]
-            float *const give = reinterpret_cast<float *>(lds.k[0]) + wr * (PP * 32);
-            static_assert(RW * PP * 32 * sizeof(float) <= sizeof(lds.k) + sizeof(lds.v), "room for it");
+            float *const give = reinterpret_cast<float *>(scratch) + wr * (PP * 32);
+            static_assert(RW * PP * 32 * sizeof(float) <= sizeof(lds.t[0]), "room for it");
             {
                 const int r = wr * 32 + col;
                 if (wk == 1) {
@@ -292,30 +295,29 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
                 __syncthreads();
             }
         }
-        // The results turned round in LDS, half of the columns at a time: a lane's row becomes runs of 16-byte pieces of rows.
-        constexpr int QS = PP / 8;                     // pieces of four columns of half a row
-        float *const turn = reinterpret_cast<float *>(lds.k[0]) + wr * (32 * PP / 2);
-        static_assert(RW * 16 * PP * sizeof(float) <= sizeof(lds.k) + sizeof(lds.v), "room for it");
+        // The results turned round in LDS, a quarter of the columns at a time: a lane's row becomes runs of 16-byte pieces of rows.
+        constexpr int QS = PP / 16;                    // pieces of four columns of a quarter of a row
+        float *const turn = reinterpret_cast<float *>(scratch) + wr * (32 * PP / 4);
+        static_assert(RW * 8 * PP * sizeof(float) <= sizeof(lds.t[0]), "room for it");
         if (wk == 0) {
             const int r0 = row0 + wr * 32;
             const float by = !direct ? 1.f : dead ? 0.f : 1.f / l;
             if (!direct && half == 0 && r0 + col < rows) sp.sums[slot + wr * 32 + col] = make_float2(m, bad ? -(float)attn_code(bad) : l);
 #pragma unroll
-            for (int hp = 0; hp < 2; ++hp) {
+            for (int hp = 0; hp < 4; ++hp) {
+                constexpr int ES = PP / 8;             // accumulators of a quarter: 16 of a block of 32 columns, or 8
+                const floatx16 &v = o[hp * ES / 16];
 #pragma unroll
-                for (int p = 0; p < NPB / 2; ++p)
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const floatx16 &v = o[hp * (NPB / 2) + p];
-                        const int piece = p * 8 + e / 2 + half;
-                        *reinterpret_cast<float4 *>(turn + (col * QS + (piece ^ (col & (QS - 1)))) * 4) = make_float4(v[e] * by, v[e + 1] * by, v[e + 2] * by, v[e + 3] * by);
-                    }
+                for (int e = 0; e < ES; e += 4) {
+                    const int f = hp * ES % 16 + e, piece = e / 2 + half;
+                    *reinterpret_cast<float4 *>(turn + (col * QS + (piece ^ (col & (QS - 1)))) * 4) = make_float4(v[f] * by, v[f + 1] * by, v[f + 2] * by, v[f + 3] * by);
+                }
                 wave_sync();
 #pragma unroll
                 for (int x = 0; x < 32 * QS / 64; ++x) {
                     const int y = x * 64 + lane2, r = y / QS, piece = y % QS, row = r0 + r;
                     const float4 v = *reinterpret_cast<const float4 *>(turn + (r * QS + (piece ^ (r & (QS - 1)))) * 4);
-                    const int c = hp * (PP / 2) + piece * 4;
+                    const int c = hp * (PP / 4) + piece * 4;
                     if (row >= rows) continue;
                     if (direct) {
                         const int i = sp.group.quotient(row), h = g * R + row - i * R;
@@ -334,17 +336,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void attn_tile_kernel(AttnArgs a, 
     }
 }
 
-template <int PP, int RW>
+template <int PP, int RW, int TH, int NB>
 void launch_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, hipStream_t st) {
     const unsigned grid = (unsigned)((sp.workers + 7) / 8 * 8) * (unsigned)sp.tiles;
-    hipLaunchKernelGGL((attn_tile_kernel<PP, RW>), dim3(grid), dim3(kTileThreads), 0, st, a, KvView<bf16_t>(kv), sp);
+    hipLaunchKernelGGL((attn_tile_kernel<PP, RW, TH, NB>), dim3(grid), dim3(TH), 0, st, a, KvView<bf16_t>(kv), sp);
 }
 
 }  // namespace
 
 hipError_t launch_attn_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, int rows, hipStream_t st) {
-    if (kv.headdim == 64) rows == 128 ? launch_tile<64, 4>(a, kv, sp, st) : launch_tile<64, 8>(a, kv, sp, st);
-    else rows == 128 ? launch_tile<128, 4>(a, kv, sp, st) : launch_tile<128, 8>(a, kv, sp, st);
+    if (kv.headdim == 64) rows == 64 ? launch_tile<64, 2, 256, 2>(a, kv, sp, st) : launch_tile<64, 8, 512, 3>(a, kv, sp, st);
+    else rows == 64 ? launch_tile<128, 2, 256, 2>(a, kv, sp, st) : launch_tile<128, 8, 512, 3>(a, kv, sp, st);
     return hipGetLastError();
 }
 
