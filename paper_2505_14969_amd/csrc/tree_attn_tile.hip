@@ -17,8 +17,15 @@ namespace {
 constexpr float kSlack = 8.f;
 constexpr int kKeys = 64;                            // keys of a tile
 
-// Rows of K are 16-byte pieces, permuted by the key, so that eight lanes that read the same piece of keys that follow one
-// another in S^T use all banks; 16 tokens of V are rows of 32 bytes, whose halves change places every four rows.
+// Sixteen lanes that follow one another read 16 bytes each of different rows in one cycle if they are different 16 bytes of 256
+// (64 banks).  So the 16-byte pieces of a row of K are permuted by the key's place in S^T, and the two halves of a row of 16
+// tokens of V change places every eight rows.  (Every four rows, and keys by three bits: 8.4 million cycles of conflicts for 16
+// trees of 64 nodes behind 4000 tokens, now none.)
+template <int PP>
+__device__ __forceinline__ int key_swizzle(int key) {
+    const int row = (key & 3) | ((key >> 1) & 4) | ((key << 1) & 8);         // its row of S^T, within 16
+    return PP == 128 ? row : row >> 1;                                        // (rows of 128 bytes: two to a line of banks)
+}
 template <int PP, int NB>
 struct TileLds {
     static constexpr int kTile = kKeys * PP;         // elements
@@ -57,11 +64,11 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     // where a lane's operands lie
     const int ktok = (col & 3) | ((col >> 1) & 4) | ((col << 1) & 8) | (col & 16);      // S^T row -> key
     // (row r = 4 h + e of a block of 16 holds key 8 h + e, row 8 + 4 h + e key 8 h + 4 + e)
-    const int kx = half ^ ((ktok & 3) | ((ktok >> 1) & 4));
-    int kget[4];
+    const int kx = half ^ key_swizzle<PP>(ktok);
+    int kget[NC];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) kget[c] = ktok * PP + ((2 * c) ^ kx) * 8;
-    const int vget = col * 16 + (half ^ ((col >> 2) & 1)) * 8;
+    for (int c = 0; c < NC; ++c) kget[c] = ktok * PP + ((2 * c) ^ kx) * 8;
+    const int vget = col * 16 + (half ^ ((col >> 3) & 1)) * 8;
 
     int k0 = 0, k1 = 0, whole = 0, end = 0;
     PageWalk<bf16_t> walk;
@@ -74,10 +81,10 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int y = x * WAVES + wave;
-            const int r = y * (64 / KR) + lane / KR, piece = (lane % KR) ^ ((r & 3) | ((r >> 1) & 4));
+            const int r = y * (64 / KR) + lane / KR, piece = (lane % KR) ^ key_swizzle<PP>(r);
             const int tk = t + ((y * (64 / KR)) & ~15), pk = walk.at(min(tk >> shift, end - 1));
             load_to_lds(kv.k + ((size_t)pk * kv.heads + at.g) * block + (size_t)((t + r) & mask) * PP + piece * 8, &lds.t[buf][0][y * 512]);
-            const int run = y / VR, p = (y % VR) * 32 + (lane >> 1), vhalf = (lane & 1) ^ ((p >> 2) & 1);
+            const int run = y / VR, p = (y % VR) * 32 + (lane >> 1), vhalf = (lane & 1) ^ ((p >> 3) & 1);
             const int tv = t + 16 * run, pv = walk.at(min(tv >> shift, end - 1));
             load_to_lds(kv.v + ((size_t)pv * kv.heads + at.g) * block + ((size_t)p << shift) + (tv & mask) + vhalf * 8, &lds.t[buf][1][y * 512]);
         }
@@ -140,7 +147,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 // Values behind the last node are no numbers anybody wrote.
                 for (int y = tid; y < kKeys * PP / 8; y += TH) {
                     bf16x8 *const at8 = reinterpret_cast<bf16x8 *>(lds.t[buf][1]) + y;
-                    const int run = y / (2 * PP), p = y % (2 * PP) >> 1, left = len + a.n - (t + 16 * run + ((y ^ (p >> 2)) & 1) * 8);
+                    const int run = y / (2 * PP), p = y % (2 * PP) >> 1, left = len + a.n - (t + 16 * run + ((y ^ (p >> 3)) & 1) * 8);
                     bf16x8 f = *at8;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -212,7 +219,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 for (int e = 0; e < 16; ++e) s[e] = 0.f;
                 bf16x8 kf[NC], vf[2][NPB];
 #pragma unroll
-                for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const bf16x8 *>(kt + kget[c & 3] + (c >> 2) * 64 + kb * 32 * PP);
+                for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const bf16x8 *>(kt + kget[c] + kb * 32 * PP);
                 __builtin_amdgcn_sched_barrier(0);     // (all operands requested before the first product, not one by one)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], s, 0, 0, 0);
