@@ -52,8 +52,10 @@ bool resolve(int64_t &stride, int64_t row) {
     return stride >= row && stride <= (1LL << 40) / 8;
 }
 
-int check_pool(const stree_kv *kv, const stree_pool *pool, int32_t batch) {
-    if (!pool || !pool->held || !pool->refs || !pool->free || !pool->nfree || !kv->table) return STREE_ERR_NULL_ARG;
+int check_pool(const stree_kv *kv, const stree_pool *pool, int32_t batch, bool idle) {
+    if (!pool) return STREE_ERR_NULL_ARG;
+    if (idle) return batch < 0 || batch > 4096 ? STREE_ERR_BAD_SHAPE : STREE_OK;      // (empty arrays may be null)
+    if (!pool->held || !pool->refs || !pool->free || !pool->nfree || !kv->table) return STREE_ERR_NULL_ARG;
     if (batch < 0 || batch > 4096 || (int64_t)batch * kv->max_pages > (1LL << 29)) return STREE_ERR_BAD_SHAPE;
     return STREE_OK;
 }
@@ -97,10 +99,10 @@ int stree_tree_rope(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     stree_attn a = *attn;
     if (a.rotary_dim < 0 || a.rotary_dim > kv->headdim || a.rotary_dim % 2 != 0) return STREE_ERR_BAD_SHAPE;
     if (!(a.eps >= 0.f)) return STREE_ERR_BAD_SHAPE;
+    if (a.batch == 0) return STREE_OK;                 // (empty arrays may be null)
     if (!lengths || !q || !k || !v || !q_out || !kv->k || !kv->v || !kv->table || (a.rotary_dim && !turns)) return STREE_ERR_NULL_ARG;
     const int64_t qr = (int64_t)a.nheads * kv->headdim, kr = (int64_t)kv->nheads_kv * kv->headdim;
     if (!resolve(a.q_stride_n, qr) || !resolve(a.k_stride_n, kr) || !resolve(a.v_stride_n, kr)) return STREE_ERR_BAD_STRIDE;
-    if (a.batch == 0) return STREE_OK;
     const size_t e = kv->io_dtype == STREE_BF16 ? 2 : 4, out = span(a, qr, qr, e);
     if ((overlap(q_out, out, q, span(a, a.q_stride_n, qr, e)) && !(q_out == q && a.q_stride_n == qr)) ||
         overlap(q_out, out, k, span(a, a.k_stride_n, kr, e)) || overlap(q_out, out, v, span(a, a.v_stride_n, kr, e)))
@@ -122,12 +124,12 @@ int stree_tree_attn(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     if (!rc) rc = check_heads(attn, kv);
     if (rc) return rc;
     stree_attn a = *attn;
+    if (!std::isfinite(a.softmax_scale)) return STREE_ERR_BAD_SHAPE;
+    if (a.batch == 0) return STREE_OK;
     if (!lengths || !q || !out || !kv->k || !kv->v || !kv->table) return STREE_ERR_NULL_ARG;
     const int64_t row = (int64_t)a.nheads * kv->headdim;
     if (!resolve(a.q_stride_n, row)) return STREE_ERR_BAD_STRIDE;
-    if (!std::isfinite(a.softmax_scale)) return STREE_ERR_BAD_SHAPE;
     if (a.softmax_scale == 0.f) a.softmax_scale = (float)(1.0 / std::sqrt((double)kv->headdim));
-    if (a.batch == 0) return STREE_OK;
     const size_t need = stree::tree_attn_workspace(a, *kv);
     if (need && !workspace) return STREE_ERR_NULL_ARG;
     if (need > workspace_bytes || (need && (uintptr_t)workspace % 16)) return STREE_ERR_BAD_SHAPE;
@@ -142,8 +144,8 @@ int stree_commit_kv(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     int rc = check_kv(kv, false);
     if (!rc) rc = check_nodes(attn, !parent);
     if (rc) return rc;
-    if (!accepted || !lengths || !lengths_out || !kv->k || !kv->v || !kv->table) return STREE_ERR_NULL_ARG;
     if (attn->batch == 0) return STREE_OK;
+    if (!accepted || !lengths || !lengths_out || !kv->k || !kv->v || !kv->table) return STREE_ERR_NULL_ARG;
     const size_t n = (size_t)attn->batch * sizeof(int32_t);
     if (lengths_out != lengths && overlap(lengths, n, lengths_out, n)) return STREE_ERR_BAD_ALIAS;
     return hip_status(stree::launch_commit_kv(*attn, *kv, parent, accepted, lengths, lengths_out, seq_status,
@@ -153,21 +155,21 @@ int stree_commit_kv(const stree_attn *attn, const stree_kv *kv, const int32_t *p
 int stree_resize_kv(const stree_kv *kv, const stree_pool *pool, int32_t batch, const int32_t *tokens, int32_t *seq_status,
                     void *hip_stream) {
     int rc = check_kv(kv, false);
-    if (!rc) rc = check_pool(kv, pool, batch);
+    if (!rc) rc = check_pool(kv, pool, batch, batch == 0);
     if (rc) return rc;
-    if (!tokens) return STREE_ERR_NULL_ARG;
     if (batch == 0) return STREE_OK;
+    if (!tokens) return STREE_ERR_NULL_ARG;
     return hip_status(stree::launch_resize_kv(*kv, *pool, batch, tokens, seq_status, (hipStream_t)hip_stream));
 }
 
 int stree_fork_kv(const stree_kv *kv, const stree_pool *pool, int32_t batch, int32_t nforks, const int32_t *src, const int32_t *dst,
                   int32_t *lengths, int32_t *fork_status, void *hip_stream) {
     int rc = check_kv(kv, false);
-    if (!rc) rc = check_pool(kv, pool, batch);
+    if (!rc) rc = check_pool(kv, pool, batch, nforks == 0);
     if (rc) return rc;
     if (nforks < 0 || nforks > 4096) return STREE_ERR_BAD_SHAPE;
-    if (!src || !dst || !lengths || !fork_status || !kv->k || !kv->v) return STREE_ERR_NULL_ARG;
     if (nforks == 0) return STREE_OK;
+    if (!src || !dst || !lengths || !fork_status || !kv->k || !kv->v) return STREE_ERR_NULL_ARG;
     return hip_status(stree::launch_fork_kv(*kv, *pool, batch, nforks, src, dst, lengths, fork_status, (hipStream_t)hip_stream));
 }
 

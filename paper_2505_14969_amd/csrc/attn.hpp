@@ -19,6 +19,12 @@ struct AttnArgs {
 template <typename Frag>
 __device__ __forceinline__ Frag signed_query(Frag q, float scale) { return scale < 0.f ? -q : q; }
 
+// Factor of sums that were relative to the maximum m when the maximum is `top` >= m.  Never zero: an infinity among the sums,
+// an infinite value that a row sees, stays one; what FLT_MIN leaves of anything else is nothing.
+__device__ __forceinline__ float rescale(float m, float top) {
+    return m == top ? 1.f : fmaxf(__builtin_amdgcn_exp2f(m - top), 1.17549435e-38f);
+}
+
 // sum + the values of a bf16 operand
 __device__ __forceinline__ float sum_of(bf16x8 v, float sum) {
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));

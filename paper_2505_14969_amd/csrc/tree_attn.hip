@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kThreads) void attn_plain_kernel(AttnArgs a, KvView
             if (!live) continue;
             // (NaN is in no maximum, and reaches the sum through exp2)
             const float above = fmaxf(top, wave_max(s)), base = above == -INFINITY ? 0.f : above;
-            const float p = seen ? exp2f(s - base) : 0.f, keep = top == -INFINITY ? 0.f : exp2f(top - base);
+            const float p = seen ? exp2f(s - base) : 0.f, keep = rescale(top, above);
             top = above;
             sum = sum * keep + wave_sum(p);
             prob[wave][lane] = p;

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 for (int mb = 0; mb < MB; ++mb) {
                     float v = fmaxf(top[mb], __shfl_xor(top[mb], 16));
                     v = fmaxf(m[mb], fmaxf(v, __shfl_xor(v, 32)));
-                    const float b2 = v == -INFINITY ? 0.f : v, keep = m[mb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mb] - b2);
+                    const float b2 = v == -INFINITY ? 0.f : v, keep = rescale(m[mb], v);
                     m[mb] = v, base[mb] = b2;
                     l[mb] *= keep;
 #pragma unroll
@@ -312,8 +312,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             float top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][r][0]);
-            // (rows without a finite score: their sums stay what they are)
-            keep[mb] = m[mb] == top ? 1.f : m[mb] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mb] - top);
+            keep[mb] = rescale(m[mb], top);
         }
         const bool dead = len < 0 || bad != 0;
         const size_t slot = ((size_t)(worker + unit) * sp.tiles + tile) * sp.rows;
@@ -335,8 +334,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][r][0]);
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) {
-                    const float mw = ml[w][r][0], f = mw == top ? 1.f : mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-                    all += ml[w][r][1] * f;
+                    all += ml[w][r][1] * rescale(ml[w][r][0], top);
                     v += *reinterpret_cast<const floatx4 *>(&lds.o[w][r][c - c0]);
                 }
                 if (direct) {
@@ -396,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
 #pragma unroll
             for (int s = 0; s < kFewParts; ++s)
                 if (s < plan.y) {
-                    const float f = w[s].x == top ? 1.f : w[s].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w[s].x - top);
+                    const float f = rescale(w[s].x, top);
                     sum += w[s].y * f;
                     v.x = fmaf(p[s].x, f, v.x), v.y = fmaf(p[s].y, f, v.y), v.z = fmaf(p[s].z, f, v.z), v.w = fmaf(p[s].w, f, v.w);
                 }
@@ -438,7 +436,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
                     const size_t slot = slot0 + s * step;
                     const float2 w = sp.sums[slot];
                     const float4 p = *reinterpret_cast<const float4 *>(sp.parts + slot * P + 4 * c);
-                    const float f = w.x == top ? 1.f : w.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.x - top);
+                    const float f = rescale(w.x, top);
                     sum += w.y * f;
                     v.x = fmaf(p.x, f, v.x), v.y = fmaf(p.y, f, v.y), v.z = fmaf(p.z, f, v.z), v.w = fmaf(p.w, f, v.w);
                 }

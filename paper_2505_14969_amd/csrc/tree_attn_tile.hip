@@ -242,7 +242,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 if (__builtin_expect(__any(above), 0)) {
             {
                         const float v = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-                        const float b2 = v == -INFINITY ? 0.f : v, keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - b2);
+                        const float b2 = v == -INFINITY ? 0.f : v, keep = rescale(m, v);
                         m = v, base = b2;
                         l *= keep;
 #pragma unroll
@@ -289,9 +289,8 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 __syncthreads();
                 if (wk == 0) {
                     const float m2 = ml[r][0], hi = fmaxf(m, m2);
-                    // (rows without a finite score: their sums stay what they are)
-                    const float f1 = m == hi ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - hi);
-                    const float f2 = m2 == hi ? 1.f : m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - hi);
+                    const float f1 = rescale(m, hi);
+                    const float f2 = rescale(m2, hi);
                     m = hi;
                     l = l * f1 + ml[r][1] * f2;
 #pragma unroll
