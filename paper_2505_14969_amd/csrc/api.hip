@@ -74,7 +74,7 @@ size_t span_bytes(int64_t rows, int64_t stride, int64_t row, size_t elem) {
 
 extern "C" {
 
-int stree_version(void) { return 2; }
+int stree_version(void) { return 3; }
 
 size_t stree_workspace_bytes(const stree_dims *dims) {
     // every intermediate of every kernel lives in LDS or registers: no entry point needs device scratch

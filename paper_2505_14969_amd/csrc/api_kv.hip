@@ -46,10 +46,11 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 size_t span(const stree_attn &a, int64_t stride, int64_t row, size_t e) {
     return a.batch > 0 ? (size_t)(((int64_t)a.batch * a.nnodes - 1) * stride + row) * e : 0;
 }
-// 0 = dense; a row has to fit
-bool resolve(int64_t &stride, int64_t row) {
+// 0 = dense; a row has to fit, and the rows of all sequences have to lie within 2^60 bytes
+bool resolve(int64_t &stride, int64_t row, const stree_attn &a) {
     if (stride == 0) stride = row;
-    return stride >= row && stride <= (1LL << 40) / 8;
+    int64_t all;
+    return stride >= row && !__builtin_mul_overflow(stride, (int64_t)a.batch * a.nnodes, &all) && all <= 1LL << 58;
 }
 
 int check_pool(const stree_kv *kv, const stree_pool *pool, int32_t batch, bool idle) {
@@ -102,7 +103,7 @@ int stree_tree_rope(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     if (a.batch == 0) return STREE_OK;                 // (empty arrays may be null)
     if (!lengths || !q || !k || !v || !q_out || !kv->k || !kv->v || !kv->table || (a.rotary_dim && !turns)) return STREE_ERR_NULL_ARG;
     const int64_t qr = (int64_t)a.nheads * kv->headdim, kr = (int64_t)kv->nheads_kv * kv->headdim;
-    if (!resolve(a.q_stride_n, qr) || !resolve(a.k_stride_n, kr) || !resolve(a.v_stride_n, kr)) return STREE_ERR_BAD_STRIDE;
+    if (!resolve(a.q_stride_n, qr, a) || !resolve(a.k_stride_n, kr, a) || !resolve(a.v_stride_n, kr, a)) return STREE_ERR_BAD_STRIDE;
     const size_t e = kv->io_dtype == STREE_BF16 ? 2 : 4, out = span(a, qr, qr, e);
     if ((overlap(q_out, out, q, span(a, a.q_stride_n, qr, e)) && !(q_out == q && a.q_stride_n == qr)) ||
         overlap(q_out, out, k, span(a, a.k_stride_n, kr, e)) || overlap(q_out, out, v, span(a, a.v_stride_n, kr, e)))
@@ -128,7 +129,7 @@ int stree_tree_attn(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     if (a.batch == 0) return STREE_OK;
     if (!lengths || !q || !out || !kv->k || !kv->v || !kv->table) return STREE_ERR_NULL_ARG;
     const int64_t row = (int64_t)a.nheads * kv->headdim;
-    if (!resolve(a.q_stride_n, row)) return STREE_ERR_BAD_STRIDE;
+    if (!resolve(a.q_stride_n, row, a)) return STREE_ERR_BAD_STRIDE;
     if (a.softmax_scale == 0.f) a.softmax_scale = (float)(1.0 / std::sqrt((double)kv->headdim));
     const size_t need = stree::tree_attn_workspace(a, *kv);
     if (need && !workspace) return STREE_ERR_NULL_ARG;

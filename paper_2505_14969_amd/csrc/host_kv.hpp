@@ -46,6 +46,14 @@ stree_kv make_kv(Arg k_cache, Arg v_cache, Arg table, bool layers) {
 const int32_t *make_parent(Arg parent, int64_t B, int64_t N) {
     return numbers_or_none(parent, {B, N}, "parent int32 [B,N], dense, or None for a chain");
 }
+// Element stride between the tokens of [B,N,heads,headdim] rows.  0 means dense to the library, so rows that lie on one another
+// (an expanded tensor) are refused; of a single row the stride means nothing.
+int64_t rows_stride(const Array &t, int64_t B, int64_t N) {
+    const int64_t s = token_stride(t, N);
+    if (B * N <= 1) return 0;
+    require(s >= t.size(2) * t.size(3), "rows apart from one another");
+    return s;
+}
 float number_of(PyObject *o) {
     const double v = PyFloat_AsDouble(o);
     if (PyErr_Occurred()) throw Raised{};
@@ -74,7 +82,7 @@ PyObject *rope(const Args &a) {
     }
     for (const Arg &w : {a[q_norm], a[k_norm]})
         if (w.o != Py_None) require(Array(w).shaped({P}) && Array(w).same_type(tq) && Array(w).is_contiguous(), "norm weights [P] in q's dtype");
-    d.q_stride_n = token_stride(tq, N), d.k_stride_n = token_stride(tk, N), d.v_stride_n = token_stride(tv, N);
+    d.q_stride_n = rows_stride(tq, B, N), d.k_stride_n = rows_stride(tk, B, N), d.v_stride_n = rows_stride(tv, B, N);
     const int32_t *p0 = make_parent(a[parent], B, N), *p1 = numbers(a[lengths], {B}, "lengths int32 [B]");
     int32_t *p2 = numbers_or_none(a[status], {B}, "status int32 [B]");
     Result o;
@@ -101,7 +109,7 @@ PyObject *attn(const Args &a) {
         d.softmax_scale = number_of(a[scale]);
         require(d.softmax_scale != 0.f, "a scale other than 0");
     }
-    d.q_stride_n = token_stride(tq, N);
+    d.q_stride_n = rows_stride(tq, B, N);
     const int32_t *p0 = make_parent(a[parent], B, N), *p1 = numbers(a[lengths], {B}, "lengths int32 [B]");
     int32_t *p2 = numbers_or_none(a[status], {B}, "status int32 [B]");
     Result o;

@@ -550,9 +550,9 @@ hipError_t launch(const AttnArgs &a, const stree_attn &at, const stree_kv &kv, v
 bool attn_stream_supported(const stree_attn &a, const stree_kv &kv, const void *q, const void *out) {
     const int e = kv.io_dtype == STREE_BF16 ? 8 : 4;
     if (kv.headdim % e || a.q_stride_n % e || (((uintptr_t)q | (uintptr_t)out | (uintptr_t)kv.k | (uintptr_t)kv.v) % 16)) return false;
-    // grid dimensions: workgroups, and units in the joining kernel
+    // grid dimensions: workgroups (of up to 512 threads), and units in the joining kernel
     const Shape s(a, kv);
-    return ((int64_t)s.workers + 8) * s.tiles < (1 << 24) && (int64_t)a.batch * kv.nheads_kv < 65536;
+    return ((int64_t)s.workers + 8) * s.tiles < (1 << 23) && (int64_t)a.batch * kv.nheads_kv < 65536;
 }
 
 size_t attn_stream_workspace(const stree_attn &a, const stree_kv &kv) {

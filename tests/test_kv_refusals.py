@@ -89,7 +89,7 @@ def test_abi_refusals(lib):
         assert call(lib, kv={"nlayers": 2}) == SHAPE
         assert call(lib, parent=NULL, a={"batch": 256, "nnodes": 1 << 23}) == SHAPE      # batch * nodes * heads from 2^31 on
         assert call(lib, a={"q_stride_n": H * P - 1}) == STRIDE and call(lib, a={"q_stride_n": -H * P}) == STRIDE
-        assert call(lib, a={"q_stride_n": 1 << 60}) == STRIDE
+        assert call(lib, a={"q_stride_n": 1 << 60}) == STRIDE and call(lib, a={"q_stride_n": 1 << 56}) == STRIDE
         assert call(lib, q=NULL) == ARG and call(lib, out=NULL) == ARG
         rows = B * N * H * P * 2
         for q in (AT + 0x8000000 + 2, AT + 0x8000000 - rows + 2, AT + 0x8000000 + rows - 2):
@@ -202,6 +202,8 @@ REFUSED += [
     ("stree_tree_rope", "q", lambda t: t[0], ValueError), ("stree_tree_rope", "q", lambda t: t.float(), AssertionError), ("stree_tree_rope", "q", _strided, AssertionError),
     ("stree_tree_rope", "q", lambda t: t.numpy(force=True) if t.dtype != BF else np.zeros(t.shape), (TypeError, AttributeError)),
     ("stree_tree_rope", "k", lambda t: t[:, :, :1], AssertionError), ("stree_tree_rope", "v", lambda t: t.float(), AssertionError), ("stree_tree_rope", "v", _strided, AssertionError),
+    ("stree_tree_rope", "q", lambda t: t[:, :1].expand(B, N, H, P), AssertionError),      # rows that lie on one another
+    ("stree_tree_rope", "k", lambda t: t[:1, :1].expand(B, N, G, P), AssertionError), ("stree_tree_attn", "q", lambda t: t[:1, :1].expand(B, N, H, P), AssertionError),
     ("stree_tree_rope", "turns", lambda t: t.float(), AssertionError), ("stree_tree_rope", "turns", lambda t: torch.zeros(P, dtype=torch.float64), AssertionError),
     ("stree_tree_rope", "q_norm", lambda t: t[:-1], AssertionError), ("stree_tree_rope", "k_norm", lambda t: t.float(), AssertionError),
     ("stree_tree_rope", "out", lambda t: torch.zeros(B, N, H, P), AssertionError), ("stree_tree_rope", "out", lambda t: torch.zeros(B, N, H, 2 * P, dtype=BF)[..., :P], AssertionError),
