@@ -41,15 +41,20 @@ constexpr int kTileKeys = 128;         // keys that the work is counted in: a st
 
 // The work of a call is B sequences x heads x tiles of their keys, which the device alone knows how many there are of: every
 // worker (a workgroup, or one for each tile of rows) takes an equal share of the tiles in that order, so that lengths may
-// differ as they like, and a sequence's head is cut where a share ends.  Parts of a head that was cut go to scratch, slot
-// (worker + unit): going on to the next part raises one of the two, or both.
+// differ as they like, and a sequence's head is cut where a share ends.  Parts of a head that was cut go to scratch, which has
+// two slots a worker: only the first head of a share can have begun in an earlier one (slot 2 w), and only the last can go on
+// (slot 2 w + 1).
 struct AttnSplit {
     int workers, tiles, rows, batch;   // tiles of rows; rows: kept of each (fewer than the tile's where there is only one)
     Divisor group;                     // query heads of a key/value head
     int2 *plan;                        // [units]: first worker of the unit and how many, written by the first
-    float2 *sums;                      // [workers + units, tiles, rows]: (top, sum of 2^(s - top)); a negative sum: -attn_code()
-    float *parts;                      // [workers + units, tiles, rows, dim]: sums of 2^(s - top) V
+    float2 *sums;                      // [2 workers, tiles, rows]: (top, sum of 2^(s - top)); a negative sum: -attn_code()
+    float *parts;                      // [2 workers, tiles, rows, dim]: sums of 2^(s - top) V
     explicit AttnSplit(int r) : group(r) {}
+    // row 0 of a worker's part of a tile of rows: of a head that begins there, or of one that began before
+    __device__ __forceinline__ size_t part(int worker, bool begins, int tile) const {
+        return ((size_t)(2 * worker + begins) * tiles + tile) * rows;
+    }
 };
 
 // A value that all lanes of a wave have alike, for the compiler to keep it once.

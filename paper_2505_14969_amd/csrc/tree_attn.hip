@@ -40,8 +40,8 @@ __global__ __launch_bounds__(kThreads) void attn_plain_kernel(AttnArgs a, KvView
     const T *const q = static_cast<const T *>(a.q);
     T *const out = static_cast<T *>(a.out);
     const int rows = a.n * a.heads;
-    for (int r0 = blockIdx.x * (kThreads / 64); r0 < rows; r0 += gridDim.x * (kThreads / 64)) {
-        const int r = r0 + wave;
+    for (long r0 = blockIdx.x * (kThreads / 64); r0 < rows; r0 += gridDim.x * (kThreads / 64)) {
+        const int r = (int)min(r0 + wave, (long)INT32_MAX);
         if (r >= rows) continue;
         const int i = r / a.heads, h = r % a.heads, g = h / R;
         const size_t token = (size_t)b * a.n + i;

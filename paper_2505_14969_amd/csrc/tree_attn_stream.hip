@@ -166,8 +166,8 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
         // tiles [t0, t1) of head g of sequence b
         const int b = at.b, g = at.g, len = at.len, w1 = k1, col = again(lane) & 15, grp = again(lane) >> 4, vtok = E * grp;
         const int unit = b * kv.heads + g;
-        const bool direct = at.whole();
-        if (at.t0 == 0 && sp.plan && tile == 0 && threadIdx.x == 0)
+        const bool direct = at.whole(), begins = at.t0 == 0;
+        if (begins && sp.plan && tile == 0 && threadIdx.x == 0)
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
         if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_nodes(lds.index.tree, lds.index.bits, a.parent, b, a.n, (a.n + 31) / 32);
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             keep[mb] = rescale(m[mb], top);
         }
         const bool dead = len < 0 || bad != 0;
-        const size_t slot = ((size_t)(worker + unit) * sp.tiles + tile) * sp.rows;
+        const size_t slot = sp.part(worker, begins, tile);
         for (int c0 = 0; c0 < PP; c0 += SL) {
             if (c0) __syncthreads();
 #pragma unroll
@@ -367,12 +367,11 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
     if (plan.y == 1) return;
     const int g = unit % kv.heads, b = unit / kv.heads, rows = a.n * R;
     const int quads = P / 4, over = kThreads / quads, c = tid % quads, s0 = tid / quads;
-    const size_t step = (size_t)sp.tiles * sp.rows;
+    auto slot_of = [&](int tile, int r, int s) { return sp.part(plan.x + s, s == 0, tile) + r; };
     if (plan.y <= kFewParts) {
         if (s0 >= over) return;
         for (int row = blockIdx.x * over + s0; row < rows; row += gridDim.x * over) {
             const int tile = row / tile_rows, r = row - tile * tile_rows;
-            const size_t slot0 = ((size_t)(plan.x + unit) * sp.tiles + tile) * sp.rows + r;
             float2 w[kFewParts];
             float4 p[kFewParts];
             float top = -INFINITY, code = -INFINITY;
@@ -380,8 +379,9 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
             for (int s = 0; s < kFewParts; ++s) {
                 w[s] = make_float2(-INFINITY, 0.f);
                 if (s < plan.y) {
-                    w[s] = sp.sums[slot0 + s * step];
-                    p[s] = *reinterpret_cast<const float4 *>(sp.parts + (slot0 + s * step) * P + 4 * c);
+                    const size_t slot = slot_of(tile, r, s);
+                    w[s] = sp.sums[slot];
+                    p[s] = *reinterpret_cast<const float4 *>(sp.parts + slot * P + 4 * c);
                 }
             }
 #pragma unroll
@@ -408,11 +408,10 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
     }
     for (int row = blockIdx.x; row < rows; row += gridDim.x) {
         const int tile = row / tile_rows, r = row - tile * tile_rows;
-        const size_t slot0 = ((size_t)(plan.x + unit) * sp.tiles + tile) * sp.rows + r;
         // maximum of all parts, or what one of them found wrong (a negative sum)
         float top = -INFINITY, code = -INFINITY;
         for (int s = tid; s < plan.y; s += kThreads) {
-            const float2 v = sp.sums[slot0 + s * step];
+            const float2 v = sp.sums[slot_of(tile, r, s)];
             top = fmaxf(top, v.x);
             if (v.y < 0.f) code = fmaxf(code, v.y);
         }
@@ -433,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
             if (s0 < over) {
 #pragma unroll 4
                 for (int s = s0; s < plan.y; s += over) {
-                    const size_t slot = slot0 + s * step;
+                    const size_t slot = slot_of(tile, r, s);
                     const float2 w = sp.sums[slot];
                     const float4 p = *reinterpret_cast<const float4 *>(sp.parts + slot * P + 4 * c);
                     const float f = rescale(w.x, top);
@@ -468,7 +467,7 @@ struct Shape {
         const int64_t units = (int64_t)a.batch * kv.nheads_kv, most = units * (((int64_t)kv.max_pages * kv.page + kTileKeys - 1) / kTileKeys);
         shared = kv.io_dtype == STREE_BF16 && (kv.headdim == 64 || kv.headdim == 128) && rows > 32;
         if (shared) {
-            blocks = rows <= 64 ? 4 : 16;
+            blocks = rows <= 128 ? 4 : 16;
             tiles = (rows + 16 * blocks - 1) / (16 * blocks);
             const int chip = blocks == 4 ? 2 * kChip : kChip, w = chip / tiles < 1 ? 1 : chip / tiles;
             workers = (int)(w < most ? w : most);
@@ -496,10 +495,10 @@ AttnSplit split_of(const stree_attn &a, const stree_kv &kv) {
     return s;
 }
 
-// scratch: plan, sums, parts, each on 16 bytes; none where every unit has one tile
+// scratch: plan, sums, parts, each on 16 bytes; none where nothing can be cut, with one worker or one tile a unit
 size_t lay_out(AttnSplit &s, const stree_attn &a, const stree_kv &kv, void *workspace) {
-    if ((int64_t)kv.max_pages * kv.page <= kTileKeys) return 0;
-    const size_t units = (size_t)a.batch * kv.nheads_kv, slots = (units + s.workers) * s.tiles * s.rows;
+    if (s.workers == 1 || (int64_t)kv.max_pages * kv.page <= kTileKeys) return 0;
+    const size_t units = (size_t)a.batch * kv.nheads_kv, slots = (size_t)2 * s.workers * s.tiles * s.rows;
     const size_t plan = (units * sizeof(int2) + 15) / 16 * 16, sums = (slots * sizeof(float2) + 15) / 16 * 16;
     char *at = static_cast<char *>(workspace);
     s.plan = reinterpret_cast<int2 *>(at);

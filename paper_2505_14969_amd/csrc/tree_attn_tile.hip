@@ -44,6 +44,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     constexpr int WAVES = TH / 64, ROWS = 32 * RW, KW = WAVES / RW, KB = 2 / KW, NC = PP / 16, NPB = PP / 32;    // key waves; blocks of 32 keys a wave
     constexpr int LOADS = kKeys * PP / 512 / WAVES;                                   // a wave's loads of 1 KB for a tile's keys, and for its values
     static_assert(KW * KB == 2, "64 keys a tile");
+    static_assert(sizeof(TreeLds) <= 2 * kKeys * PP * sizeof(bf16_t), "the tree is looked at in a tile's place");
     typedef TileLds<PP, NB> Lds;
     __shared__ Lds lds;
     __shared__ float ml[KW > 1 ? ROWS : 1][2];
@@ -114,8 +115,8 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     enter();
     for (;;) {
         const int b = at.b, g = at.g, len = at.len, w1 = k1, unit = b * kv.heads + g;
-        const bool direct = at.whole();
-        if (at.t0 == 0 && sp.plan && tile == 0 && tid == 0)
+        const bool direct = at.whole(), begins = at.t0 == 0;
+        if (begins && sp.plan && tile == 0 && tid == 0)
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
         if (whole > len && len >= 0 && whole > 0 && a.parent) {
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         {
         const int lane2 = again(lane), col = lane2 & 31, half = lane2 >> 5;
         const bool dead = len < 0 || bad != 0;
-        const size_t slot = ((size_t)(worker + unit) * sp.tiles + tile) * sp.rows;
+        const size_t slot = sp.part(worker, begins, tile);
         l += __shfl_xor(l, 32);
         if constexpr (KW > 1) {
             // the second half of the keys is handed to the first's waves, 32 rows at a time: [wave][p][row]
