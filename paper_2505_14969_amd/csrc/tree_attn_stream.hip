@@ -75,6 +75,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     const float scale = fabsf(a.scale);
     Share at = Share::start(a, kv, sp, worker, lds.first);
     if (worker >= at.workers) return;
+    if (sp.batch > 64) __syncthreads();                // (its numbers lay where the tree goes)
 
     // What the waves are at: the piece's keys up to k1 (these rows see no more of it) and `whole` (where it ends), the page
     // numbers, the queries, and the keys and values of the next step, always on their way.  The waves take the piece's steps
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
         if (begins && sp.plan && tile == 0 && threadIdx.x == 0)
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
-        if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_nodes(lds.index.tree, lds.index.bits, a.parent, b, a.n, (a.n + 31) / 32);
+        if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_paths(lds.index.tree, lds.index.bits, a.parent, b, a.n);
 
         float m[MB], base[MB], l[MB];
         floatx4 o[MB][NP];

@@ -66,9 +66,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     const int ktok = (col & 3) | ((col >> 1) & 4) | ((col << 1) & 8) | (col & 16);      // S^T row -> key
     // (row r = 4 h + e of a block of 16 holds key 8 h + e, row 8 + 4 h + e key 8 h + 4 + e)
     const int kx = half ^ key_swizzle<PP>(ktok);
-    int kget[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) kget[c] = ktok * PP + ((2 * c) ^ kx) * 8;
+    const int kget = ktok * PP + kx * 8;               // (chunk c of 16 columns: ^ 16 c)
     const int vget = col * 16 + (half ^ ((col >> 3) & 1)) * 8;
 
     int k0 = 0, k1 = 0, whole = 0, end = 0;
@@ -79,6 +77,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     auto fetch = [&](int t, int buf) {
         walk.reach(kv, at.b, t >> shift, end, lane);
         constexpr int KR = PP / 8, VR = PP / 32;       // pieces of a row of K; loads of a run of V
+        const int lane = again(tid) & 63;
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int y = x * WAVES + wave;
@@ -119,10 +118,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         if (begins && sp.plan && tile == 0 && tid == 0)
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
-        if (whole > len && len >= 0 && whole > 0 && a.parent) {
-            bad = index_nodes(*reinterpret_cast<TreeLds *>(scratch), lds.bits, a.parent, b, a.n, words);
-            __syncthreads();
-        }
+        if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_paths(*reinterpret_cast<TreeLds *>(scratch), lds.bits, a.parent, b, a.n);
         const int col = again(lane) & 31, half = again(lane) >> 5;
         float m, base, l;
         floatx16 o[NPB];
@@ -136,13 +132,46 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
         }
         int buf = 0;
-        for (int t = k0; t < w1; t += kKeys, buf = buf == NB - 1 ? 0 : buf + 1) {
+        floatx16 s;                                    // of the wave's next 32 keys, always a step ahead
+        float top = -INFINITY;
+        bf16x8 kf[NC];
+        const int mine = wk * KB * 32 * PP;            // (this wave's keys of a tile)
+        auto load_k = [&](int from, int kb) {
+            const int at8 = again(kget) + mine + from * 2 * Lds::kTile + kb * 32 * PP;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const bf16x8 *>(lds.t[0][0] + (at8 ^ (16 * c)));
+        };
+        auto product = [&]() {
+            floatx16 r;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) r = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], r, 0, 0, 0);
+            return r;
+        };
+        auto largest = [&](const floatx16 &v) {
+            float r = v[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) r = fmaxf(r, v[e]);
+            return r;
+        };
+        // This wave's part of tile t is there; up to `behind` tiles that follow it may be on their way.
+        auto arrived = [&](int t, int behind) {
+            if (behind >= 2 && t + 2 * kKeys < w1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * LOADS) : "memory");
+            else if (behind >= 1 && t + kKeys < w1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        };
+        if (k0 < w1) {
+            arrived(k0, NB - 2);
+            if (k0 + (NB - 1) * kKeys < w1) fetch(k0 + (NB - 1) * kKeys, NB - 1);
+            load_k(0, 0);
+            s = product();
+            top = largest(s);
+        }
+        for (int t = k0; t < w1; t += kKeys) {
             const bool tail = t + kKeys > len || t + kKeys > w1;
-            // This wave's part of the tile is there (younger loads, those of the next tile, may be on their way), and with the
-            // barrier everybody's; everybody is done with the tile before this one, whose place the next to be fetched takes.
-            if (NB > 2 && t + kKeys < w1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-            if (t + (NB - 1) * kKeys < w1) fetch(t + (NB - 1) * kKeys, buf == 0 ? NB - 1 : buf - 1);
+            const bf16_t *const vt = lds.t[buf][1] + mine;
+            uint32_t seen[KB];                         // 16 keys a block and lane: bits 0 - 7 of its first 16, 8 - 15 of its last
             int odd = 0;
             if (__builtin_expect(tail, 0)) {
                 // Values behind the last node are no numbers anybody wrote.
@@ -158,11 +187,6 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                     *at8 = f;
                 }
                 odd = __syncthreads_or(odd);
-            }
-
-            const bf16_t *const kt = lds.t[buf][0] + wk * 32 * PP, *const vt = lds.t[buf][1] + wk * 32 * PP;
-            uint32_t seen[KB];                      // 16 keys a block and lane: bits 0 - 7 of its first 16, 8 - 15 of its last
-            if (__builtin_expect(tail, 0)) {
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) {
                         seen[kb] = 0;
@@ -213,43 +237,40 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                     __syncthreads();
                 }
             }
+            const int after = buf == NB - 1 ? 0 : buf + 1;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {          // 32 keys
-                floatx16 s;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 0.f;
-                bf16x8 kf[NC], vf[2][NPB];
-#pragma unroll
-                for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const bf16x8 *>(kt + kget[c] + kb * 32 * PP);
-                __builtin_amdgcn_sched_barrier(0);     // (all operands requested before the first product, not one by one)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], q[c], s, 0, 0, 0);
+                bf16x8 vf[2][NPB];
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
                     for (int p = 0; p < NPB; ++p) vf[y][p] = *reinterpret_cast<const bf16x8 *>(vt + (2 * kb + y) * 16 * PP + vget + p * 32 * 16);
-                __builtin_amdgcn_sched_barrier(0);
+                if (kb < KB - 1) {
+                    load_k(buf, kb + 1);
+                } else if (t + kKeys < w1) {
+                    // This wave has this tile's last operands, and its part of the next tile is there (younger loads, those of the
+                    // tiles behind it, may be on their way); with the barrier that holds for everybody, and the tile's place is free.
+                    arrived(t + kKeys, NB - 2);
+                    if (t + NB * kKeys < w1) fetch(t + NB * kKeys, buf);
+                    load_k(after, 0);
+                }
                 if (__builtin_expect(tail, 0)) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         if (!((seen[kb] >> e) & 1u)) s[e] = -INFINITY;
+                    top = largest(s);
                 }
-                bool above = false;
-                float top = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
                 top *= scale;
-                above |= top > m + kSlack;
-                if (__builtin_expect(__any(above), 0)) {
-            {
-                        const float v = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-                        const float b2 = v == -INFINITY ? 0.f : v, keep = rescale(m, v);
-                        m = v, base = b2;
-                        l *= keep;
+                if (__builtin_expect(__any(top > m + kSlack), 0)) {
+                    const float v = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                    const float b2 = v == -INFINITY ? 0.f : v, keep = rescale(m, v);
+                    m = v, base = b2;
+                    l *= keep;
 #pragma unroll
-                        for (int p = 0; p < NPB; ++p) o[p] *= keep;
-                    }
+                    for (int p = 0; p < NPB; ++p) o[p] *= keep;
                 }
+                // the products of the next 32 keys (of none behind the last, of old ones) go along with these keys' exponentials
+                const floatx16 next = product();
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     // one rounding of each probability; their sum is the rounded ones'
@@ -260,7 +281,10 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
 #pragma unroll
                     for (int p = 0; p < NPB; ++p) o[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[y][p], pf, o[p], 0, 0, 0);
                 }
+                s = next;
+                top = largest(s);
             }
+            buf = after;
         }
         // (pages of the piece that only later rows see)
         int missing = walk.bad;
@@ -352,8 +376,8 @@ void launch_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, hip
 }  // namespace
 
 hipError_t launch_attn_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, int rows, hipStream_t st) {
-    if (kv.headdim == 64) rows == 64 ? launch_tile<64, 2, 256, 2>(a, kv, sp, st) : launch_tile<64, 8, 512, 3>(a, kv, sp, st);
-    else rows == 64 ? launch_tile<128, 2, 256, 2>(a, kv, sp, st) : launch_tile<128, 8, 512, 3>(a, kv, sp, st);
+    if (kv.headdim == 64) rows == 64 ? launch_tile<64, 2, 256, 2>(a, kv, sp, st) : launch_tile<64, 8, 512, 4>(a, kv, sp, st);
+    else rows == 64 ? launch_tile<128, 2, 256, 2>(a, kv, sp, st) : launch_tile<128, 8, 512, 4>(a, kv, sp, st);
     return hipGetLastError();
 }
 
