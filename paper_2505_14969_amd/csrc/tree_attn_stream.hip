@@ -1,6 +1,6 @@
 // The tuned kernel of stree_tree_attn: the cache streamed once from memory straight into operand registers.
 //
-// A workgroup takes 16, 32 or 64 query rows (node, head) of one key/value head and one piece of the sequence's keys; its
+// A workgroup takes 16 or 32 query rows (node, head) of one key/value head and one piece of the sequence's keys; its
 // four waves take the piece's keys in turn, STEP at a time.  Products are formed transposed, so that in
 // every accumulator a lane owns one query row (column lane % 16):
 //   S^T = K Q^T,   P = 2^(S - m),   O^T += V^T P^T
@@ -9,7 +9,10 @@
 // barrier and no shuffle in the loop: the maximum is moved only when a score passes it by kSlack (2^kSlack is harmless in
 // fp32), which a vote finds out.  Waves are joined through LDS at the end, pieces by a second kernel.
 //
-// Bound by memory: 16 rows take 256 cycles of the matrix unit per 32 keys where the chip's memory needs 5000 to bring them.
+// Bound by memory: 16 rows take 256 cycles of the matrix unit per 32 keys where the chip's memory needs 5000 to bring them.  Heads
+// of 128 in bf16, 4 rows of 8 key/value heads: 64 sequences of up to 4096 tokens 116 us (671 MB, 5.8 TB/s), one of 131071 100 us
+// (537 MB, 5.4 TB/s); a read of nothing but such pages reaches 6.8 TB/s here.  fp32, 60 rows behind 500 tokens: 16.7 us, of which
+// 3.9 join parts, the rest is the chain launch -> lengths -> pages -> keys -> products.
 #include "attn.hpp"
 
 namespace stree {
@@ -54,7 +57,9 @@ struct StreamShape {
     static constexpr int kRows = 16 * MB;
     static constexpr int kSlice = PP * kRows <= 2048 ? PP : 2048 / kRows;        // columns joined at a time: 32 KB of LDS
     static constexpr int kLd = kSlice + 4;
-    static constexpr int kMinWaves = PP * MB <= 256 ? 2 : 1;                     // waves on a SIMD: as many registers as that leaves
+    // Waves on a SIMD: one where a head's operands need more than half of the registers (64 sequences of 2000 tokens, heads of
+    // 256: 175 us, with two 295), else two (32 rows of 128, 16 sequences of 2000 tokens: 40 us, with one 49).
+    static constexpr int kMinWaves = PP <= 128 ? 2 : 1;
 };
 
 template <typename T, int PP, int MB, bool WHOLE>
@@ -460,6 +465,12 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
 
 // Rows of a workgroup, in blocks of 16, and workers: as many rows as there are, up to what the registers hold, unless the
 // keys that the table has room for would then leave CUs idle; as many workers as the chip holds workgroups at once.
+//
+// Which kernel, bf16 heads of 128: from 33 rows on the one that shares tiles (64 sequences of 4000 tokens, 64 rows: 209 us, here in
+// two tiles 300; 16 of 2000, 36 rows: 46 and 50; 32 rows: 46, here 40).  Only one short sequence is better off here (60 rows behind
+// 500 tokens: 19 and 15 us).  Tiles of 64 rows up to 128, of 256 beyond (16 sequences of 2000 tokens, 128 rows in two tiles 62 us, in
+// half of one 70; 192 rows in three 119, in one 69).  Here one tile of 32 rows rather than two of 16: 64 sequences of 4000 tokens
+// 170 us, not 276.
 struct Shape {
     int blocks, tiles, workers;
     bool shared;                                     // the kernel that shares tiles of keys through LDS
@@ -477,8 +488,7 @@ struct Shape {
         blocks = rows <= 16 ? 1 : 2;
         while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
         tiles = (rows + 16 * blocks - 1) / (16 * blocks);
-        const int regs = blocks * (kv.headdim <= 64 ? 64 : kv.headdim <= 128 ? 128 : 256);       // (as in StreamShape)
-        int64_t w = kChip * (regs <= 256 ? 2 : 1) / tiles;
+        int64_t w = kChip * (kv.headdim <= 128 ? 2 : 1) / tiles;                     // (kMinWaves)
         if (w < 1) w = 1;
         workers = (int)(w < most ? w : most);
     }

@@ -1,13 +1,20 @@
-// The kernel of stree_tree_attn for many query rows: 128 or 256 rows (node, head) of one key/value head share every tile of
+// The kernel of stree_tree_attn for many query rows: 64 or 256 rows (node, head) of one key/value head share every tile of
 // 64 keys through LDS, products on the bf16 matrix units.
 //
-// With 256 rows a key of 512 bytes comes with 131072 operations: memory and the matrix units need about the same time, and the
-// exponentials (a quarter of the vector rate) nearly as much again, so everything has to overlap: eight waves, two on a SIMD,
-// of 32 rows each.  (64 rows a wave would halve the operands read from LDS, which need as long as the products; but with 256
-// values in accumulators the compiler spills what is on its way from memory: 16 trees of 64 nodes 199 us where this takes 84.)  As in the streaming kernel a lane owns a query row in every
-// accumulator (S^T = K Q^T, O^T += V^T P^T), keys stand in S^T in the order that makes the probabilities the operand of the
-// second product, and the maximum moves only when a score passes it by kSlack.  Tiles go from memory straight into LDS, the
-// next one or two on their way behind the products: one barrier a tile.
+// As in the streaming kernel a lane owns a query row in every accumulator (S^T = K Q^T, O^T += V^T P^T), keys stand in S^T in the
+// order that makes the probabilities the operand of the second product, and the maximum moves only when a score passes it by
+// kSlack.  A wave has 32 rows, and two waves are on a SIMD: 256 rows are eight waves side by side; 64 rows are two, and two more
+// take the other half of a tile's keys, with two such workgroups on a CU.  Tiles go from memory straight into LDS, up to three on
+// their way; one barrier a tile.  The first product of the next 32 keys is issued with the exponentials of these, which it does
+// not wait for.
+//
+// With 256 rows a tile takes 2048 cycles of a SIMD's matrix unit, about as many of LDS reads and as many of exponentials and sums.
+// What bounds it is the chip's power: at 64 rows of 131000 tokens (537 MB) the clock falls to 1.6 GHz, and a tile takes 2.25 us;
+// where the keys come from L2 (less to move) 1.6.  Short calls keep 1.9 GHz and spend 10 us on the chain to the first tile and
+// 12 us on parts: 16 trees of 64 nodes behind 2900 tokens on average 95 us (44.6 Gflop, 190 MB), of which 12 join parts; two
+// prompts of 512 behind 1537 80 us.  Tried beside this: 64 rows a wave, half the LDS reads, one wave a SIMD (138 us where this took
+// 99: accumulators move between two register files), 128 rows and two workgroups a CU (108 and 97), the streaming hint (the
+// prompts: 88 and 80, tiles of rows share keys in L2).
 #include "attn.hpp"
 
 namespace stree {
@@ -101,13 +108,11 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         if (k0 >= k1) return;
         end = ((k1 - 1) >> shift) + 1;
         walk.start(kv, at.b, k0 >> shift, end, lane);
-            {
-            const int r = row0 + wr * 32 + col, rr = min(r, rows - 1), i = sp.group.quotient(rr), h = at.g * R + rr - i * R;
-            const bf16_t *src = static_cast<const bf16_t *>(a.q) + ((size_t)at.b * a.n + i) * a.q_sn + (size_t)h * PP + half * 8;
+        const int r = min(row0 + wr * 32 + col, rows - 1), i = sp.group.quotient(r), h = at.g * R + r - i * R;
+        const bf16_t *src = static_cast<const bf16_t *>(a.q) + ((size_t)at.b * a.n + i) * a.q_sn + (size_t)h * PP + half * 8;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) q[c] = signed_query(*reinterpret_cast<const bf16x8 *>(src + c * 16), a.scale);
-        }
-#pragma unroll
+        for (int c = 0; c < NC; ++c) q[c] = signed_query(*reinterpret_cast<const bf16x8 *>(src + c * 16), a.scale);
+#pragma unroll 1
         for (int x = 0; x < NB - 1; ++x)
             if (k0 + x * kKeys < k1) fetch(k0 + x * kKeys, x);
     };
@@ -120,17 +125,13 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         int bad = len >= 0 && !kv.fits((int64_t)len + a.n) ? STREE_SEQ_LENGTH : 0;
         if (whole > len && len >= 0 && whole > 0 && a.parent) bad = index_paths(*reinterpret_cast<TreeLds *>(scratch), lds.bits, a.parent, b, a.n);
         const int col = again(lane) & 31, half = again(lane) >> 5;
-        float m, base, l;
+        const int node = sp.group.quotient(min(row0 + wr * 32 + col, rows - 1));
+        float m = -INFINITY, base = 0.f, l = 0.f;
         floatx16 o[NPB];
-        int node;
-            {
-            node = sp.group.quotient(min(row0 + wr * 32 + col, rows - 1));
-            m = -INFINITY, base = 0.f, l = 0.f;
 #pragma unroll
-            for (int p = 0; p < NPB; ++p)
+        for (int p = 0; p < NPB; ++p)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
-        }
+            for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
         int buf = 0;
         floatx16 s;                                    // of the wave's next 32 keys, always a step ahead
         float top = -INFINITY;
@@ -188,16 +189,16 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                 }
                 odd = __syncthreads_or(odd);
 #pragma unroll
-                    for (int kb = 0; kb < KB; ++kb) {
-                        seen[kb] = 0;
+                for (int kb = 0; kb < KB; ++kb) {
+                    seen[kb] = 0;
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int t8 = t + (wk * KB + kb) * 32 + y * 16 + half * 8, left = w1 - t8;
-                            uint32_t v = seen_nodes<8>(lds.bits, words, a.parent != nullptr, node, t8 - len);
-                            v &= left >= 8 ? 0xffu : left > 0 ? (1u << left) - 1u : 0u;
-                            seen[kb] |= v << (8 * y);
-                        }
+                    for (int y = 0; y < 2; ++y) {
+                        const int t8 = t + (wk * KB + kb) * 32 + y * 16 + half * 8, left = w1 - t8;
+                        uint32_t v = seen_nodes<8>(lds.bits, words, a.parent != nullptr, node, t8 - len);
+                        v &= left >= 8 ? 0xffu : left > 0 ? (1u << left) - 1u : 0u;
+                        seen[kb] |= v << (8 * y);
                     }
+                }
                 if (__builtin_expect(odd, 0)) {
                     // Infinities and NaN among the values of nodes: zero probabilities would not keep them from the rows that do
                     // not see the node.  They are counted per row, and are zeros for the products below.
@@ -213,21 +214,19 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
                                 up[e] = (bf16_t)((float)v[e] < INFINITY ? 0.f : 1.f);              // +inf, NaN
                                 down[e] = (bf16_t)((float)v[e] > -INFINITY ? 0.f : 1.f);           // -inf, NaN
                             }
-            {
-                                const uint32_t bits = (KB > 1 && kb ? seen[KB - 1] : seen[0]) >> (8 * (y & 1));
-                                bf16x8 see;
+                            const uint32_t bits = (KB > 1 && kb ? seen[KB - 1] : seen[0]) >> (8 * (y & 1));
+                            bf16x8 see;
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) see[e] = (bf16_t)((bits >> e) & 1u ? 1.f : 0.f);
-                                floatx16 cu, cd;
+                            for (int e = 0; e < 8; ++e) see[e] = (bf16_t)((bits >> e) & 1u ? 1.f : 0.f);
+                            floatx16 cu, cd;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) cu[e] = cd[e] = 0.f;
-                                cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, see, cu, 0, 0, 0);
-                                cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, see, cd, 0, 0, 0);
+                            for (int e = 0; e < 16; ++e) cu[e] = cd[e] = 0.f;
+                            cu = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, see, cu, 0, 0, 0);
+                            cd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, see, cd, 0, 0, 0);
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) {
-                                    if (cu[e] > 0.f) o[p][e] += INFINITY;
-                                    if (cd[e] > 0.f) o[p][e] -= INFINITY;
-                                }
+                            for (int e = 0; e < 16; ++e) {
+                                if (cu[e] > 0.f) o[p][e] += INFINITY;
+                                if (cd[e] > 0.f) o[p][e] -= INFINITY;
                             }
                         }
                     }
@@ -302,29 +301,27 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
             // the second half of the keys is handed to the first's waves, 32 rows at a time: [wave][p][row]
             float *const give = reinterpret_cast<float *>(scratch) + wr * (PP * 32);
             static_assert(RW * PP * 32 * sizeof(float) <= sizeof(lds.t[0]), "room for it");
-            {
-                const int r = wr * 32 + col;
-                if (wk == 1) {
-                    if (half == 0) ml[r][0] = m, ml[r][1] = l;
+            const int r = wr * 32 + col;
+            if (wk == 1) {
+                if (half == 0) ml[r][0] = m, ml[r][1] = l;
 #pragma unroll
-                    for (int p = 0; p < NPB; ++p)
+                for (int p = 0; p < NPB; ++p)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] = o[p][e];
-                }
-                __syncthreads();
-                if (wk == 0) {
-                    const float m2 = ml[r][0], hi = fmaxf(m, m2);
-                    const float f1 = rescale(m, hi);
-                    const float f2 = rescale(m2, hi);
-                    m = hi;
-                    l = l * f1 + ml[r][1] * f2;
-#pragma unroll
-                    for (int p = 0; p < NPB; ++p)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[p][e] = o[p][e] * f1 + give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] * f2;
-                }
-                __syncthreads();
+                    for (int e = 0; e < 16; ++e) give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] = o[p][e];
             }
+            __syncthreads();
+            if (wk == 0) {
+                const float m2 = ml[r][0], hi = fmaxf(m, m2);
+                const float f1 = rescale(m, hi);
+                const float f2 = rescale(m2, hi);
+                m = hi;
+                l = l * f1 + ml[r][1] * f2;
+#pragma unroll
+                for (int p = 0; p < NPB; ++p)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[p][e] = o[p][e] * f1 + give[(p * 32 + 8 * (e >> 2) + 4 * half + (e & 3)) * 32 + col] * f2;
+            }
+            __syncthreads();
         }
         // The results turned round in LDS, a quarter of the columns at a time: a lane's row becomes runs of 16-byte pieces of rows.
         constexpr int QS = PP / 16;                    // pieces of four columns of a quarter of a row
