@@ -72,6 +72,16 @@ def _fork(lib, kv=None, pool=None, batch=B, forks=F, src=AT, dst=AT, lengths=AT,
     return lib.stree_fork_kv(C.byref(_kv(**(kv or {}))), _pool(**(pool or {})), batch, forks, src, dst, lengths, status, None)
 
 
+@pytest.mark.parametrize("N,heads", [(1, 8), (16, 8), (64, 32), (2048, 32), (1 << 18, 8)])
+def test_scratch_does_not_grow_with_the_batch(lib, N, heads):
+    """Parts of rows that were cut: as many as the chip holds at once, whatever the number of sequences."""
+    need = [lib.stree_attn_workspace_bytes(C.byref(_attn(batch=b, nnodes=N, nheads=heads)), C.byref(_kv(nheads_kv=8, headdim=128, max_pages=1 << 14)))
+            for b in (8, 64, 256)]
+    units = [8 * 8, 64 * 8, 256 * 8]
+    assert need[0] == 0 or [n - 8 * u for n, u in zip(need, units)] == [need[0] - 8 * units[0]] * 3
+    assert max(need) <= 2 * 512 * 256 * (128 + 2) * 4 + 8 * units[2] + 32
+
+
 def test_abi_refusals(lib):
     for call in (_rope, _att, _commit, _resize, _fork):
         for kv, rc in KV_BAD:
