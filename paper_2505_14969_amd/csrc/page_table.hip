@@ -2,10 +2,10 @@
 // call does depends on the order of rows and entries alone: a page given back by several rows at once is put on the stack by
 // the first of its entries, found by an atomic minimum over the entries' numbers in refs[] itself.
 //
-// A few thousand numbers at most: bound by the chain of dependent phases (reads, atomics in L2, barriers).  64 rows that drop 30
-// pages each and 16 of them growing: 11 and 5 us (kernel times); 48 forks of 8 layers with 8 heads of 128, pages of 32 tokens: 9 us
-// for the numbers and 14.5 for 105 MB of pages, 7.2 TB/s.  Each phase looks up four entries of a thread at once: one at a time the
-// same drop took 17 us.
+// A few thousand numbers at most: bound by the chain of dependent phases (reads, atomics in L2, barriers).  48 rows that drop up to
+// 33 pages each 11 us, 64 that take one or two 5; 48 forks in 8 layers of 8 heads of 128, pages of 32 tokens: 9 us for the numbers
+// and 14.5 for the pages (some 100 MB read and written, 6.9 TB/s).  Each phase of a drop looks up four entries of a thread at once:
+// one at a time the same drop took 17 us.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 
