@@ -2,7 +2,7 @@
 //   x^ = x / sqrt(mean x^2 + eps) * w;  pairs (u, w) turn by 2 pi frac(position * turns[j]), frac in 64 bits
 // Rows are read once and written once: bound by memory where there are many, two fp32 prompts of 2047 tokens with 32 + 8 + 8 heads of
 // 128 40 us (201 MB, 5.0 TB/s); else by the chain length -> tree, pages -> angles -> rows: one token 5.7 us, 16 trees of 64 nodes
-// 13.3 us (25 MB, 6 us at that rate), of which about 2 are angles that every group of heads works out for itself.
+// 13.3 us (25 MB, 6 us at that rate); the angles, which every group of heads works out for itself, are 0.6 of them.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 
