@@ -46,11 +46,18 @@ constexpr int kTileKeys = 128;         // keys that the work is counted in: a st
 // (slot 2 w + 1).
 struct AttnSplit {
     int workers, tiles, rows, batch;   // tiles of rows; rows: kept of each (fewer than the tile's where there is only one)
+    bool spread;                       // a worker's tiles of rows are spread over the XCDs, not on one of them
     Divisor group;                     // query heads of a key/value head
     int2 *plan;                        // [units]: first worker of the unit and how many, written by the first
     float2 *sums;                      // [2 workers, tiles, rows]: (top, sum of 2^(s - top)); a negative sum: -attn_code()
     float *parts;                      // [2 workers, tiles, rows, dim]: sums of 2^(s - top) V
     explicit AttnSplit(int r) : group(r) {}
+    // What a workgroup is: worker, and which of its workgroups.  On one XCD the tiles of rows share the keys and values through its
+    // L2; spread out they fill the chip whatever their number.  (Workgroups go to the eight XCDs in turn.)
+    unsigned grid() const { return (unsigned)(spread ? workers : (workers + 7) / 8 * 8) * (unsigned)tiles; }
+    __device__ __forceinline__ int2 place(unsigned x) const {
+        return spread ? make_int2((int)x / tiles, (int)x % tiles) : make_int2(((int)(x >> 3) / tiles) * 8 + (int)(x & 7), (int)(x >> 3) % tiles);
+    }
     // row 0 of a worker's part of a tile of rows: of a head that begins there, or of one that began before
     __device__ __forceinline__ size_t part(int worker, bool begins, int tile) const {
         return ((size_t)(2 * worker + begins) * tiles + tile) * rows;
@@ -167,6 +174,9 @@ struct Share {
         return s;
     }
     __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
+    // Which of `n` tiles of rows the workgroup `of` a worker's takes here: of every other head the last ones first, since of a long
+    // chain the last rows see twice as many keys as the average (a prompt of 8192 tokens: 630 us, without 1095).
+    __device__ __forceinline__ int row_tile(int heads, int of, int n) const { return (b * heads + g) & 1 ? n - 1 - of : of; }
     // on to the next head or sequence; false at the end of the share
     template <typename T>
     __device__ __forceinline__ bool next(const AttnArgs &a, const KvView<T> &kv) {

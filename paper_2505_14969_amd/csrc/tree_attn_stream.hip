@@ -72,10 +72,10 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     __shared__ union { Index index; float o[kWaves][ROWS][LD]; int64_t first[kThreads + 1]; } lds;
     __shared__ float ml[kWaves][ROWS][2];
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), P = kv.dim;
-    // The row tiles of one worker follow one another on one XCD, whose L2 they share the keys and values through.
-    const int tile = (int)(blockIdx.x >> 3) % sp.tiles, worker = ((int)(blockIdx.x >> 3) / sp.tiles) * 8 + (int)(blockIdx.x & 7);
+    const int2 here = sp.place(blockIdx.x);
+    const int worker = here.x, group = here.y;
     if (worker >= sp.workers) return;
-    const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, mine = min(ROWS, rows - row0);
+    const int R = sp.group.d, rows = a.n * R;
     T *const out = static_cast<T *>(a.out);
     const float scale = fabsf(a.scale);
     Share at = Share::start(a, kv, sp, worker, lds.first);
@@ -139,6 +139,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     // A new piece: everything that does not wait for its first keys.
     auto enter = [&]() {
         const int col = again(lane) & 15, grp = again(lane) >> 4;
+        const int row0 = at.row_tile(kv.heads, group, sp.tiles) * ROWS;
         k0 = k1 = whole = 0;
         if (at.len >= 0 && kv.fits((int64_t)at.len + a.n)) {
             const int last = sp.group.quotient(min(row0 + ROWS, rows) - 1);
@@ -171,6 +172,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     for (;;) {
         // tiles [t0, t1) of head g of sequence b
         const int b = at.b, g = at.g, len = at.len, w1 = k1, col = again(lane) & 15, grp = again(lane) >> 4, vtok = E * grp;
+        const int tile = at.row_tile(kv.heads, group, sp.tiles), row0 = tile * ROWS, mine = min(ROWS, rows - row0);
         const int unit = b * kv.heads + g;
         const bool direct = at.whole(), begins = at.t0 == 0;
         if (begins && sp.plan && tile == 0 && threadIdx.x == 0)
@@ -188,6 +190,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
 #pragma unroll
             for (int p = 0; p < NP; ++p) o[mb][p] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
+        const int clear = min(w1, len + (a.parent ? 0 : sp.group.quotient(row0) + 1));     // all of these rows see the keys up to here
         for (int t = k0 + wave * STEP; t < w1; t += STRIDE) {
             floatx4 s[MB][KB];
 #pragma unroll
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
                 place(t + STRIDE, col, grp);
                 load_k(grp);
             }
-            const bool tail = t + STEP > len || t + STEP > w1;
+            const bool tail = t + STEP > clear;
             uint32_t seen[MB];
             float p[MB][E], top[MB];
             bool above = false;
@@ -474,6 +477,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
 struct Shape {
     int blocks, tiles, workers;
     bool shared;                                     // the kernel that shares tiles of keys through LDS
+    bool spread;                                     // (AttnSplit)
     Shape(const stree_attn &a, const stree_kv &kv) {
         const int rows = a.nnodes * (a.nheads / kv.nheads_kv);
         const int64_t units = (int64_t)a.batch * kv.nheads_kv, most = units * (((int64_t)kv.max_pages * kv.page + kTileKeys - 1) / kTileKeys);
@@ -481,15 +485,20 @@ struct Shape {
         if (shared) {
             blocks = rows <= 128 ? 4 : 16;
             tiles = (rows + 16 * blocks - 1) / (16 * blocks);
-            const int chip = blocks == 4 ? 2 * kChip : kChip, w = chip / tiles < 1 ? 1 : chip / tiles;
-            workers = (int)(w < most ? w : most);
+            crowd(blocks == 4 ? 2 * kChip : kChip, most);
             return;
         }
         blocks = rows <= 16 ? 1 : 2;
         while (blocks > 1 && most * ((rows + 16 * blocks - 1) / (16 * blocks)) < kChip) blocks /= 2;
         tiles = (rows + 16 * blocks - 1) / (16 * blocks);
-        int64_t w = kChip * (kv.headdim <= 128 ? 2 : 1) / tiles;                     // (kMinWaves)
-        if (w < 1) w = 1;
+        crowd(kChip * (kv.headdim <= 128 ? 2 : 1), most);                            // (kMinWaves)
+    }
+    // As many workers as `chip` workgroups make; on one XCD each where that leaves out an eighth of them at most (a prompt of 8192
+    // tokens, 128 tiles of rows: two workers on two of the eight XCDs took 2436 us, spread out 630).
+    void crowd(int chip, int64_t most) {
+        int w = chip / tiles < 1 ? 1 : chip / tiles;
+        spread = w / 8 * 64 < w * 7;
+        if (!spread) w &= ~7;
         workers = (int)(w < most ? w : most);
     }
 };
@@ -500,6 +509,7 @@ AttnSplit split_of(const stree_attn &a, const stree_kv &kv) {
     AttnSplit s(R);
     s.workers = shape.workers;
     s.tiles = shape.tiles;
+    s.spread = shape.spread;
     s.rows = rows < 16 * shape.blocks ? rows : 16 * shape.blocks;
     s.batch = a.batch;
     s.plan = nullptr, s.sums = nullptr, s.parts = nullptr;
@@ -520,7 +530,7 @@ size_t lay_out(AttnSplit &s, const stree_attn &a, const stree_kv &kv, void *work
 
 template <typename T, int PP, int MB>
 void launch_stream(const AttnArgs &a, const KvView<T> &kv, const AttnSplit &sp, hipStream_t st) {
-    const unsigned grid = (unsigned)((sp.workers + 7) / 8 * 8) * (unsigned)sp.tiles;
+    const unsigned grid = sp.grid();
     if (kv.dim == PP) hipLaunchKernelGGL((attn_stream_kernel<T, PP, MB, true>), dim3(grid), dim3(kThreads), 0, st, a, kv, sp);
     else hipLaunchKernelGGL((attn_stream_kernel<T, PP, MB, false>), dim3(grid), dim3(kThreads), 0, st, a, kv, sp);
 }

@@ -12,7 +12,7 @@
 // What bounds it is the chip's power: at 64 rows of 131000 tokens (537 MB) the clock falls to 1.6 GHz, and a tile takes 2.25 us;
 // where the keys come from L2 (less to move) 1.6.  Short calls keep 1.9 GHz and spend 10 us on the chain to the first tile and
 // 12 us on parts: 16 trees of 64 nodes behind 2900 tokens on average 95 us (44.6 Gflop, 190 MB), of which 12 join parts; two
-// prompts of 512 behind 1537 80 us.  Tried beside this: 64 rows a wave, half the LDS reads, one wave a SIMD (138 us where this took
+// prompts of 512 behind 1537 74 us, of which 12; one of 8192 630 us (550 Gflop, 0.88 Pflop/s).  Tried beside this: 64 rows a wave, half the LDS reads, one wave a SIMD (138 us where this took
 // 99: accumulators move between two register files), 128 rows and two workgroups a CU (108 and 97), the streaming hint (the
 // prompts: 88 and 80, tiles of rows share keys in L2).
 #include "attn.hpp"
@@ -57,9 +57,10 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     __shared__ float ml[KW > 1 ? ROWS : 1][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wr = wave % RW, wk = wave / RW;
     const int col = lane & 31, half = lane >> 5;
-    const int tile = (int)(blockIdx.x >> 3) % sp.tiles, worker = ((int)(blockIdx.x >> 3) / sp.tiles) * 8 + (int)(blockIdx.x & 7);
+    const int2 here = sp.place(blockIdx.x);
+    const int worker = here.x, group = here.y;
     if (worker >= sp.workers) return;
-    const int R = sp.group.d, rows = a.n * R, row0 = tile * ROWS, words = (a.n + 31) / 32;
+    const int R = sp.group.d, rows = a.n * R, words = (a.n + 31) / 32;
     bf16_t *const out = static_cast<bf16_t *>(a.out);
     const float scale = fabsf(a.scale);
     Share at = Share::start<TH>(a, kv, sp, worker, reinterpret_cast<int64_t *>(lds.t[0]));
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     };
     auto enter = [&]() {
         const int lane2 = again(lane), col = lane2 & 31, half = lane2 >> 5;
+        const int row0 = at.row_tile(kv.heads, group, sp.tiles) * ROWS;
         k0 = k1 = whole = 0;
         if (at.len >= 0 && kv.fits((int64_t)at.len + a.n)) {
             const int last = sp.group.quotient(min(row0 + ROWS, rows) - 1);
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
     };
     enter();
     for (;;) {
-        const int b = at.b, g = at.g, len = at.len, w1 = k1, unit = b * kv.heads + g;
+        const int b = at.b, g = at.g, len = at.len, w1 = k1, unit = b * kv.heads + g, tile = at.row_tile(kv.heads, group, sp.tiles), row0 = tile * ROWS;
         const bool direct = at.whole(), begins = at.t0 == 0;
         if (begins && sp.plan && tile == 0 && tid == 0)
             sp.plan[unit] = make_int2(worker, direct ? 1 : at.shares.worker(at.x + at.tiles - 1) - worker + 1);
@@ -132,6 +134,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         for (int p = 0; p < NPB; ++p)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[p][e] = 0.f;
+        const int clear = min(w1, len + (a.parent ? 0 : sp.group.quotient(row0) + 1));     // all of these rows see the keys up to here
         int buf = 0;
         floatx16 s;                                    // of the wave's next 32 keys, always a step ahead
         float top = -INFINITY;
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
             top = largest(s);
         }
         for (int t = k0; t < w1; t += kKeys) {
-            const bool tail = t + kKeys > len || t + kKeys > w1;
+            const bool tail = t + kKeys > clear;
             const bf16_t *const vt = lds.t[buf][1] + mine;
             uint32_t seen[KB];                         // 16 keys a block and lane: bits 0 - 7 of its first 16, 8 - 15 of its last
             int odd = 0;
@@ -366,8 +369,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
 
 template <int PP, int RW, int TH, int NB>
 void launch_tile(const AttnArgs &a, const stree_kv &kv, const AttnSplit &sp, hipStream_t st) {
-    const unsigned grid = (unsigned)((sp.workers + 7) / 8 * 8) * (unsigned)sp.tiles;
-    hipLaunchKernelGGL((attn_tile_kernel<PP, RW, TH, NB>), dim3(grid), dim3(TH), 0, st, a, KvView<bf16_t>(kv), sp);
+    hipLaunchKernelGGL((attn_tile_kernel<PP, RW, TH, NB>), dim3(sp.grid()), dim3(TH), 0, st, a, KvView<bf16_t>(kv), sp);
 }
 
 }  // namespace

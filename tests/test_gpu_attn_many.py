@@ -4,7 +4,7 @@ import pytest
 
 from kv_helpers import attn_bound, dev, within
 from paper_2505_14969_amd import binding as st
-from test_gpu_tree_attn import _case, _check, _want
+from test_gpu_tree_attn import _case, _check, _run, _want
 
 pytestmark = pytest.mark.gpu
 
@@ -22,6 +22,33 @@ def test_many_sequences_of_many_rows(B, N, R, P, page):
     c["table"][B - 1, (int(lens[B - 1]) + N - 1) // page] = 1 << 30
     c["parent"][5, N - 1] = N - 1
     _check(c, plain=(False,))
+
+
+@pytest.mark.parametrize("io,N,R,lens", [("bf16", 2100, 4, [1, 0]), ("bf16", 1100, 4, [70, -1, 3]), ("bf16", 800, 3, [0, 900]), ("f32", 700, 4, [5, 0]),
+                                         ("f32", 300, 4, [1000]), ("bf16", 130, 1, [64, 63, 65])])
+def test_long_prompts(io, N, R, lens):
+    """Tiles of rows that see ever more keys, more of them than leave a worker for every eighth of the chip."""
+    _check(_case(N, io, N, 2 * R, 2, 64, 64, lens, tree="chain"), plain=(False,))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_infinities_in_a_prompt(io):
+    """A prompt's token whose values are not finite: the rows in front of it do not see them, all others do, whatever tile they are in."""
+    c = _case(6, io, 400, 4, 1, 64, 16, [37, 20], tree="chain")
+    for node, value, col in ((100, np.inf, 3), (250, -np.inf, 3), (131, np.nan, 60), (399, np.inf, 9)):
+        t = 37 + node
+        c["v"][c["table"][0, t // 16], 0, col, t % 16] = value
+    got, status = _run(c)
+    assert not status.any()
+    with np.errstate(invalid="ignore"):
+        want, _, weight, score = _want(c)
+    for col, first in ((60, 131), (9, 399)):
+        assert np.isfinite(got[0, :first, :, col]).all() and not np.isfinite(got[0, first:, :, col]).any()
+    assert np.isfinite(got[0, :100, :, 3]).all() and (got[0, 100:250, :, 3] == np.inf).all() and np.isnan(got[0, 250:, :, 3]).all()
+    inside = np.isfinite(want)
+    assert np.array_equal(np.isfinite(got), inside)
+    bound = attn_bound(io, want, weight, score, 64, 437)
+    assert np.all(np.abs(got[inside] - want[inside]) <= bound[inside])
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
