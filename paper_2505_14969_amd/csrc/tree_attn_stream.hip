@@ -146,9 +146,8 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             k0 = at.t0 * kTileKeys, whole = min(at.t1 * kTileKeys, at.len + a.n);
             k1 = min(whole, at.len + last + 1);
         }
-        walk.bad = false;
         const int t = k0 + wave * STEP;
-        if (t >= k1) return;
+        if (t >= k1) return walk.none();
         end = ((k1 - 1) >> shift) + 1;
         walk.start(kv, at.b, t >> shift, end, lane);
         // queries: row `col` of each block, 16 bytes at column (4 c + grp) E; zeros behind the head and the last row
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
         }
         // (pages of the piece that only later rows see)
         int missing = walk.bad;
-        for (int j = (k1 >> shift) + (int)threadIdx.x; j < (whole + mask) >> shift; j += kThreads) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
+        for (int j = (k0 < k1 ? end : k0 >> shift) + (int)threadIdx.x; j < (whole + mask) >> shift; j += kThreads) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
         if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
         // the next piece's first keys are on their way while this one's waves are joined
         const bool more = at.next(a, kv);

@@ -106,8 +106,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
             k0 = at.t0 * kTileKeys, whole = min(at.t1 * kTileKeys, at.len + a.n);
             k1 = min(whole, at.len + last + 1);
         }
-        walk.bad = false;
-        if (k0 >= k1) return;
+        if (k0 >= k1) return walk.none();
         end = ((k1 - 1) >> shift) + 1;
         walk.start(kv, at.b, k0 >> shift, end, lane);
         const int r = min(row0 + wr * 32 + col, rows - 1), i = sp.group.quotient(r), h = at.g * R + r - i * R;
@@ -290,7 +289,7 @@ __global__ __launch_bounds__(TH, 2) void attn_tile_kernel(AttnArgs a, KvView<bf1
         }
         // (pages of the piece that only later rows see)
         int missing = walk.bad;
-        for (int j = (k1 >> shift) + tid; j < (whole + mask) >> shift; j += TH) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
+        for (int j = (k0 < k1 ? end : k0 >> shift) + tid; j < (whole + mask) >> shift; j += TH) missing |= !kv.exists(kv.table[(size_t)b * kv.max_pages + j]);
         if (__syncthreads_or(missing) && bad == 0) bad = STREE_SEQ_PAGE;
         const bool more = at.next(a, kv);
         if (more) enter();                             // the next piece's first tile is on its way
