@@ -442,7 +442,8 @@ int stree_tree_rope(const stree_attn *a, const stree_kv *kv, const int32_t *pare
  *   q   io [B,N,H,P] (q_stride_n)    out io [B,N,H,P] dense, must not overlap q
  * One node is one new token's step.  Long sequences are split over workgroups, whose parts a second kernel
  * joins: that takes device scratch of stree_attn_workspace_bytes(a, kv) bytes at `workspace`, aligned to 16
- * bytes (NULL where that is 0; too few bytes: STREE_ERR_BAD_SHAPE), which holds nothing between calls; calls
+ * bytes (NULL where that is 0; too few bytes: STREE_ERR_BAD_SHAPE; parts of as many rows as the chip works on at
+ * once, whatever the batch), which holds nothing between calls; calls
  * that may run at the same time need their own.  Sums, maxima and parts are fp32.  The tuned kernel rounds the
  * probabilities to bf16 for the matrix units (their sum is that of the rounded ones).
  * Infinities and NaN in the keys or values of a node reach the nodes that see it and no others.

@@ -11,10 +11,10 @@
 // With 256 rows a tile takes 2048 cycles of a SIMD's matrix unit, about as many of LDS reads and as many of exponentials and sums.
 // What bounds it is the chip's power: at 64 rows of 131000 tokens (537 MB) the clock falls to 1.6 GHz, and a tile takes 2.25 us;
 // where the keys come from L2 (less to move) 1.6.  Short calls keep 1.9 GHz and spend 10 us on the chain to the first tile and
-// 12 us on parts: 16 trees of 64 nodes behind 2900 tokens on average 95 us (44.6 Gflop, 190 MB), of which 12 join parts; two
-// prompts of 512 behind 1537 74 us, of which 12; one of 8192 630 us (550 Gflop, 0.88 Pflop/s).  Tried beside this: 64 rows a wave, half the LDS reads, one wave a SIMD (138 us where this took
-// 99: accumulators move between two register files), 128 rows and two workgroups a CU (108 and 97), the streaming hint (the
-// prompts: 88 and 80, tiles of rows share keys in L2).
+// 12 us on parts: 16 trees of 64 nodes behind 2900 tokens on average 89 to 96 us (44.6 Gflop, 190 MB), of which 12 join parts; two
+// prompts of 512 behind 1537 69 to 74 us, of which 12; one of 8192 630 us (550 Gflop, 0.88 Pflop/s).  Tried beside this: 64 rows a
+// wave, half the LDS reads, one wave a SIMD (138 us where this took 99: accumulators move between two register files), 128 rows and
+// two workgroups a CU (108 and 97), the streaming hint (the prompts: 88 and 80, tiles of rows share keys in L2).
 #include "attn.hpp"
 
 namespace stree {
