@@ -147,8 +147,8 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             k1 = min(whole, at.len + last + 1);
         }
         const int t = k0 + wave * STEP;
+        end = ((k1 - 1) >> shift) + 1;                 // (alike in all waves, those that have no keys of their own too: they share the pages behind)
         if (t >= k1) return walk.none();
-        end = ((k1 - 1) >> shift) + 1;
         walk.start(kv, at.b, t >> shift, end, lane);
         // queries: row `col` of each block, 16 bytes at column (4 c + grp) E; zeros behind the head and the last row
 #pragma unroll
