@@ -191,6 +191,16 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
         }
         const int clear = min(w1, len + (a.parent ? 0 : sp.group.quotient(row0) + 1));     // all of these rows see the keys up to here
         for (int t = k0 + wave * STEP; t < w1; t += STRIDE) {
+            if (!WHOLE) {
+                // Behind the head stand other columns of the row, which may be infinite: zeros, as the query has there.
+#pragma unroll
+                for (int c = 0; c < NK; ++c)
+#pragma unroll
+                    for (int x = 0; x < KB; ++x) {
+                        const uint4 v = __builtin_bit_cast(uint4, kf[x][c]);
+                        kf[x][c] = __builtin_bit_cast(Frag, (4 * c + grp) * E < P ? v : make_uint4(0u, 0u, 0u, 0u));
+                    }
+            }
             floatx4 s[MB][KB];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
