@@ -148,6 +148,8 @@ struct Piece<float> {
 // to HC heads of q, of k or of v).  q and k: TL lanes hold a row, 16 bytes each; a team stays with its node, whose cosines and
 // sines it keeps, and all of its rows are requested at once.  Pairs half the rotated columns apart are another lane's 16 bytes.
 // v: turned round in LDS, so that 16 bytes of a column of the tile go out at once.
+// Every workgroup looks at the page numbers of all nodes' slots before it writes; of a long prompt it then takes a tile after the
+// other, every gridDim.x-th (node_groups()).
 template <typename T, int TL, int HC, bool HALF>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv, int zq, int zk) {
     constexpr int E = Piece<T>::E, TEAMS = kThreads / TL;
@@ -156,8 +158,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
     const int b = blockIdx.y, P = kv.dim, tid = threadIdx.x, lane = tid & 63, z = blockIdx.z;
     const int len = a.lengths[b];
     const bool fits = len >= 0 && kv.fits((int64_t)len + a.n), query = z < zq, value = z >= zq + zk;
-    const int slot0 = (fits ? len & ~(kSlots - 1) : 0) + (int)blockIdx.x * kSlots, node0 = slot0 - (fits ? len : 0);     // node of slot 0
+    int slot0 = (fits ? len & ~(kSlots - 1) : 0) + (int)blockIdx.x * kSlots, node0 = slot0 - (fits ? len : 0);     // node of slot 0
     if (node0 >= a.n) return;                          // (no first tile does)
+    const int stride = (int)gridDim.x * kSlots;        // to this workgroup's next tile
     const int h0 = (query ? z : value ? z - zq - zk : z - zq) * HC, heads = min(HC, (query ? a.heads : kv.heads) - h0);
     const size_t row0 = (size_t)b * a.n;
     const long sn = query ? a.q_sn : value ? a.v_sn : a.k_sn;
@@ -171,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
         for (int h = 0; h < HC; ++h) raw[h] = *reinterpret_cast<const uint4 *>(row + (size_t)(h0 + min(h, heads - 1)) * P);
     };
     request(tid / TL);
-    const int pg = fits ? kv.page_of(b, slot0) : 0;
+    int pg = fits ? kv.page_of(b, slot0) : 0;
     int bad = 0;
     if (len >= 0) {
         if (!fits) {
@@ -189,55 +192,64 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
     const bool dead = len < 0 || bad;
     if (dead && !query) return;
     if (value) {
-        for (int h = 0; h < heads; ++h) {
-            for (int s = tid / TL; s < kSlots; s += TEAMS) {
-                const int i = node0 + s;
-                if (i >= 0 && i < a.n && c < pieces) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(src + (row0 + i) * sn + (size_t)(h0 + h) * P + col);
-                    const T *const w = reinterpret_cast<const T *>(&v);
+        for (;;) {
+            for (int h = 0; h < heads; ++h) {
+                for (int s = tid / TL; s < kSlots; s += TEAMS) {
+                    const int i = node0 + s;
+                    if (i >= 0 && i < a.n && c < pieces) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(src + (row0 + i) * sn + (size_t)(h0 + h) * P + col);
+                        const T *const w = reinterpret_cast<const T *>(&v);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) lds.v[s][col + e] = w[e];
+                        for (int e = 0; e < E; ++e) lds.v[s][col + e] = w[e];
+                    }
                 }
-            }
-            __syncthreads();
-            T *const dst = kv.value(pg, h0 + h, slot0);
-            for (int y = tid; y < P * (kSlots / E); y += kThreads) {
-                const int p = y / (kSlots / E), s = y % (kSlots / E) * E, i = node0 + s;
-                T *const to = dst + ((size_t)p << kv.shift) + s;
-                T w[E];
+                __syncthreads();
+                T *const dst = kv.value(pg, h0 + h, slot0);
+                for (int y = tid; y < P * (kSlots / E); y += kThreads) {
+                    const int p = y / (kSlots / E), s = y % (kSlots / E) * E, i = node0 + s;
+                    T *const to = dst + ((size_t)p << kv.shift) + s;
+                    T w[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = lds.v[s + e][p];
-                if (i >= 0 && i + E <= a.n) {
-                    uint4 v;
-                    __builtin_memcpy(&v, w, sizeof(v));
-                    *reinterpret_cast<uint4 *>(to) = v;
-                } else {
+                    for (int e = 0; e < E; ++e) w[e] = lds.v[s + e][p];
+                    if (i >= 0 && i + E <= a.n) {
+                        uint4 v;
+                        __builtin_memcpy(&v, w, sizeof(v));
+                        *reinterpret_cast<uint4 *>(to) = v;
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (i + e >= 0 && i + e < a.n) to[e] = w[e];
+                        for (int e = 0; e < E; ++e)
+                            if (i + e >= 0 && i + e < a.n) to[e] = w[e];
+                    }
                 }
+                __syncthreads();
             }
-            __syncthreads();
+            if (a.n - node0 <= stride) return;
+            slot0 += stride, node0 += stride;
+            pg = kv.page_of(b, slot0);
         }
-        return;
     }
     T *const out = static_cast<T *>(a.q_out);
     if (dead) {
-        for (int s = tid / TL; s < kSlots; s += TEAMS)
-            if (node0 + s >= 0 && node0 + s < a.n && c < pieces)
-                for (int h = 0; h < heads; ++h)
-                    *reinterpret_cast<uint4 *>(out + ((row0 + node0 + s) * a.heads + h0 + h) * P + c * E) = make_uint4(0u, 0u, 0u, 0u);
-        return;
-    }
-    const int half = a.rotary / 2;
-    for (int y = tid; y < kSlots * half; y += kThreads) {
-        const int s = y / half, j = y - s * half, i = node0 + s;
-        if (i >= 0 && i < a.n) {
-            const int d = a.parent ? tree.cnt[i] - 1 : i;
-            lds.turn[s][j] = rotation(a.turns[j], len + d, a.scale);
+        for (;; node0 += stride) {
+            for (int s = tid / TL; s < kSlots; s += TEAMS)
+                if (node0 + s >= 0 && node0 + s < a.n && c < pieces)
+                    for (int h = 0; h < heads; ++h)
+                        *reinterpret_cast<uint4 *>(out + ((row0 + node0 + s) * a.heads + h0 + h) * P + c * E) = make_uint4(0u, 0u, 0u, 0u);
+            if (a.n - node0 <= stride) return;
         }
     }
-    __syncthreads();
+    const int half = a.rotary / 2;
+    auto turn_nodes = [&]() {
+        for (int y = tid; y < kSlots * half; y += kThreads) {
+            const int s = y / half, j = y - s * half, i = node0 + s;
+            if (i >= 0 && i < a.n) {
+                const int d = a.parent ? tree.cnt[i] - 1 : i;
+                lds.turn[s][j] = rotation(a.turns[j], len + d, a.scale);
+            }
+        }
+        __syncthreads();
+    };
+    turn_nodes();
     // of this lane's columns: the weights, and where its pairs' other halves are
     const bool norm = query ? a.q_norm != nullptr : a.k_norm != nullptr;
     const T *const w = static_cast<const T *>(query ? a.q_norm : a.k_norm);
@@ -251,58 +263,77 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
         Piece<T>::widen(*reinterpret_cast<const uint4 *>(w + col), wo);
         Piece<T>::widen(*reinterpret_cast<const uint4 *>(w + other * E), wp);
     }
-    for (int s0 = 0; s0 < kSlots; s0 += TEAMS) {
-        const int s = s0 + tid / TL, i = node0 + s;
-        const bool there = s < kSlots && i >= 0 && i < a.n;
-        // y = r (A x + B x'), x' the pair's other half: weights, cosine and sine (its sign that of the place) of each column
-        float A[E], B[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            A[e] = wo[e], B[e] = 0.f;
-            const int x = col + e;
-            if (x < a.rotary) {
-                const float2 t = lds.turn[min(s, kSlots - 1)][HALF ? (second ? x - half : x) : x >> 1];
-                A[e] = wo[e] * t.x;
-                B[e] = (HALF ? wp[e] : wo[e ^ 1]) * ((HALF ? second : (e & 1)) ? t.y : -t.y);
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < HC; ++h) {
-            if (h >= heads) break;
-            float x[E], y[E], r = 1.f;
-            Piece<T>::widen(raw[h], x);
-            if (norm) {
-                float ss = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
-                if (c >= pieces) ss = 0.f;
-#pragma unroll
-                for (int o = TL / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-                r = 1.f / sqrtf(ss / (float)P + a.eps);
-            }
-            if (HALF) {
-                uint4 q;
-                q.x = wave_read(raw[h].x, team + other), q.y = wave_read(raw[h].y, team + other);
-                q.z = wave_read(raw[h].z, team + other), q.w = wave_read(raw[h].w, team + other);
-                Piece<T>::widen(q, y);
-            }
-            float out8[E];
+    for (;;) {
+        for (int s0 = 0; s0 < kSlots; s0 += TEAMS) {
+            const int s = s0 + tid / TL, i = node0 + s;
+            const bool there = s < kSlots && i >= 0 && i < a.n;
+            // y = r (A x + B x'), x' the pair's other half: weights, cosine and sine (its sign that of the place) of each column
+            float A[E], B[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float turned = fmaf(HALF ? y[e] : x[e ^ 1], B[e], x[e] * A[e]);
-                out8[e] = r * (col + e < a.rotary ? turned : x[e] * A[e]);
+                A[e] = wo[e], B[e] = 0.f;
+                const int x = col + e;
+                if (x < a.rotary) {
+                    const float2 t = lds.turn[min(s, kSlots - 1)][HALF ? (second ? x - half : x) : x >> 1];
+                    A[e] = wo[e] * t.x;
+                    B[e] = (HALF ? wp[e] : wo[e ^ 1]) * ((HALF ? second : (e & 1)) ? t.y : -t.y);
+                }
             }
-            if (there && c < pieces)
-                *reinterpret_cast<uint4 *>((query ? out + ((row0 + i) * a.heads + h0 + h) * P : kv.key(pg, h0 + h, slot0 + s)) + col) = Piece<T>::round(out8);
+#pragma unroll
+            for (int h = 0; h < HC; ++h) {
+                if (h >= heads) break;
+                float x[E], y[E], r = 1.f;
+                Piece<T>::widen(raw[h], x);
+                if (norm) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) ss = fmaf(x[e], x[e], ss);
+                    if (c >= pieces) ss = 0.f;
+#pragma unroll
+                    for (int o = TL / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
+                    r = 1.f / sqrtf(ss / (float)P + a.eps);
+                }
+                if (HALF) {
+                    uint4 q;
+                    q.x = wave_read(raw[h].x, team + other), q.y = wave_read(raw[h].y, team + other);
+                    q.z = wave_read(raw[h].z, team + other), q.w = wave_read(raw[h].w, team + other);
+                    Piece<T>::widen(q, y);
+                }
+                float out8[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float turned = fmaf(HALF ? y[e] : x[e ^ 1], B[e], x[e] * A[e]);
+                    out8[e] = r * (col + e < a.rotary ? turned : x[e] * A[e]);
+                }
+                if (there && c < pieces)
+                    *reinterpret_cast<uint4 *>((query ? out + ((row0 + i) * a.heads + h0 + h) * P : kv.key(pg, h0 + h, slot0 + s)) + col) = Piece<T>::round(out8);
+            }
+            if (s0 + TEAMS < kSlots) request(s + TEAMS);
         }
-        if (s0 + TEAMS < kSlots) request(s + TEAMS);
+        if (a.n - node0 <= stride) return;
+        slot0 += stride, node0 += stride;
+        pg = kv.page_of(b, slot0);
+        request(tid / TL);
+        __syncthreads();                               // (the angles are read)
+        turn_nodes();
     }
+}
+
+// Workgroups over the nodes of a sequence, which take `steps` steps, next to `others` for other heads and sequences: one a step, unless
+// there are more page numbers, all of which every workgroup looks at, than a workgroup has threads.  Then as many in all as the chip
+// holds at once, so that the time grows with a prompt and not with its square (131072 tokens of 8 + 2 + 2 heads of 128 205 us,
+// with a workgroup a tile 297; a million of one head of 16 0.41 ms and 4.6).
+inline unsigned node_groups(int n, int64_t steps, int64_t others) {
+    if (n <= 16 * kThreads) return (unsigned)steps;
+    const int64_t most = others < 2048 ? 2048 / others : 1;
+    return (unsigned)(steps < most ? steps : most);
 }
 
 template <typename T, int TL, int HC>
 void launch_tuned(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t st) {
     const int zq = (a.heads + HC - 1) / HC, zk = (kv.nheads_kv + HC - 1) / HC;
-    const dim3 grid((unsigned)((a.n + 2 * kSlots - 2) / kSlots), (unsigned)batch, (unsigned)(zq + 2 * zk));
+    const int z = zq + 2 * zk;
+    const dim3 grid(node_groups(a.n, (a.n + 2 * kSlots - 2) / kSlots, (int64_t)batch * z), (unsigned)batch, (unsigned)z);
     if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, TL, HC, false>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
     else hipLaunchKernelGGL((rope_kernel<T, TL, HC, true>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
 }
@@ -315,8 +346,7 @@ hipError_t launch(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t 
                        (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.q_norm | (uintptr_t)a.k_norm |
                          (uintptr_t)kv.k | (uintptr_t)kv.v) % 16) == 0 && a.heads <= 65535 / 2 && kv.nheads_kv <= 65535 / 4;
     if (!whole) {
-        hipLaunchKernelGGL((rope_plain_kernel<T>), dim3((unsigned)(a.n < (1 << 20) ? a.n : 1 << 20), (unsigned)batch), dim3(kThreads), 0, st, a,
-                           KvView<T>(kv));
+        hipLaunchKernelGGL((rope_plain_kernel<T>), dim3(node_groups(a.n, a.n, batch), (unsigned)batch), dim3(kThreads), 0, st, a, KvView<T>(kv));
         return hipGetLastError();
     }
     // Heads of a workgroup: two where there are few workgroups, so that a step of a few nodes is over sooner; eight bf16 heads,
