@@ -297,10 +297,22 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) p[mb][e] = __builtin_amdgcn_exp2f(fmaf(p[mb][e], scale, -base[mb]));
-                const Frag pf = M::round(p[mb]);       // bf16: one rounding of each probability, and their sum is the rounded ones'
+                const Frag pf = M::round(p[mb]);
                 l[mb] = sum_of(pf, l[mb]);
 #pragma unroll
                 for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
+                if (MB == 1 && sizeof(T) == 2) {
+                    // What the rounding left, in a second product: 16 bits of a probability.  It costs the matrix unit time that
+                    // memory leaves over (64 sequences, one token: 116 us with and without).  With 32 rows it is one rounding: the
+                    // second product would take up to 5 % there (heads of 80, two prompts of 512: 97 and 102 us), and 18 to 35 % in
+                    // the kernel of many rows.
+#pragma unroll
+                    for (int e = 0; e < E; ++e) p[mb][e] -= (float)pf[e];
+                    const Frag rest = M::round(p[mb]);
+                    l[mb] = sum_of(rest, l[mb]);
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], rest, o[mb][x]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
             if (more) load_v(col);
