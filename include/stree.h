@@ -466,7 +466,7 @@ size_t stree_attn_workspace_bytes(const stree_attn *a, const stree_kv *kv);
  *   lengths_out[b] = lengths[b] + d + 1
  * accepted[b] == -1, an idle sequence or one with a status: lengths_out[b] = lengths[b], nothing moves.
  * parent NULL: a chain, whose rows stand where they should.  Of `a` only batch and nnodes are read.
- *   lengths_out int32 [B]; MAY be lengths (STREE_ERR_BAD_ALIAS for any other overlap)
+ *   lengths_out int32 [B]; MAY be lengths or accepted (STREE_ERR_BAD_ALIAS for any other overlap with either)
  */
 int stree_commit_kv(const stree_attn *a, const stree_kv *kv, const int32_t *parent, const int32_t *accepted,
                     const int32_t *lengths, int32_t *lengths_out, int32_t *seq_status, void *hip_stream);

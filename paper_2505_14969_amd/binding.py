@@ -313,8 +313,8 @@ def stree_attn_workspace(q, k_cache, v_cache, table) -> int:
 
 def stree_commit_kv(parent, accepted, lengths, k_cache, v_cache, table, lengths_out: Optional[torch.Tensor] = None,
                     status: Optional[torch.Tensor] = None, nnodes: Optional[int] = None):
-    """Rows of the accepted path moved together, in every layer -> new lengths; lengths_out may be lengths itself.
-    A chain (parent None) says its nnodes."""
+    """Rows of the accepted path moved together, in every layer -> new lengths; lengths_out may be lengths itself or
+    accepted.  A chain (parent None) says its nnodes."""
     return _native().commit_kv(parent, accepted, lengths, k_cache, v_cache, table, lengths_out, status, nnodes)
 
 

@@ -148,7 +148,8 @@ int stree_commit_kv(const stree_attn *attn, const stree_kv *kv, const int32_t *p
     if (attn->batch == 0) return STREE_OK;
     if (!accepted || !lengths || !lengths_out || !kv->k || !kv->v || !kv->table) return STREE_ERR_NULL_ARG;
     const size_t n = (size_t)attn->batch * sizeof(int32_t);
-    if (lengths_out != lengths && overlap(lengths, n, lengths_out, n)) return STREE_ERR_BAD_ALIAS;
+    for (const int32_t *in : {lengths, accepted})
+        if (lengths_out != in && overlap(in, n, lengths_out, n)) return STREE_ERR_BAD_ALIAS;
     return hip_status(stree::launch_commit_kv(*attn, *kv, parent, accepted, lengths, lengths_out, seq_status,
                                               (hipStream_t)hip_stream));
 }

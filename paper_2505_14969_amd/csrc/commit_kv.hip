@@ -72,6 +72,7 @@ __global__ __launch_bounds__(kThreads) void commit_kv_kernel(CommitArgs a, KvVie
     const int b = blockIdx.y, tid = threadIdx.x, len = a.lengths[b], k = a.accepted[b];
     int count;
     const int bad = find_path(a, kv, tree, bits, path, b, len, k, count);
+    if (!MOVE) __syncthreads();                                  // (every wave has its length and node, where these may be written)
     if (blockIdx.x == 0 && tid == 0) {
         if (a.lengths_out) a.lengths_out[b] = len + count;
         if (a.status) a.status[b] = bad;
@@ -127,9 +128,9 @@ hipError_t launch_runs(CommitArgs a, const stree_kv &kv, int batch, hipStream_t 
     int per = (int)((places + 2047) / 2048);
     per = per < kv.nheads_kv ? per : kv.nheads_kv;
     const int chunks = (kv.nheads_kv + per - 1) / per;
-    // A chain's rows stand where they should.  Lengths that are overwritten are so when every workgroup has read them.
+    // A chain's rows stand where they should.  Lengths, and accepted nodes, that are overwritten are so when every workgroup has read them.
     const CommitArgs after = a;
-    const bool apart = !a.parent || a.lengths == a.lengths_out;
+    const bool apart = !a.parent || a.lengths == a.lengths_out || a.accepted == a.lengths_out;
     if (a.parent) {
         if (apart) a.lengths_out = a.status = nullptr;
         hipLaunchKernelGGL((commit_kv_kernel<T, true, E>), dim3((unsigned)kv.nlayers * chunks, (unsigned)batch), dim3(kThreads), 0, st, a, view,
