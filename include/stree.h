@@ -445,7 +445,7 @@ int stree_tree_rope(const stree_attn *a, const stree_kv *kv, const int32_t *pare
  * bytes (NULL where that is 0; too few bytes: STREE_ERR_BAD_SHAPE; parts of as many rows as the chip works on at
  * once, whatever the batch), which holds nothing between calls; calls
  * that may run at the same time need their own.  Sums, maxima and parts are fp32.  The tuned kernels round bf16's
- * probabilities for the matrix units (their sum is that of the rounded ones): to 16 bits where a key/value head has up to
+ * probabilities for the matrix units (their sum is that of the rounded ones): to 15 bits where a key/value head has up to
  * 16 rows (nnodes * nheads / nheads_kv), to bf16's 8 where there are more.
  * Infinities and NaN in the keys or values of a node reach the nodes that see it and no others.
  * Tuned kernels: headdim a multiple of 8 (bf16) or 4 (fp32), 16-byte aligned q, k, v, out and a q stride of whole

@@ -68,6 +68,12 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
     typedef typename M::Frag Frag;
     typedef StreamShape<T, PP, MB> Shape;
     constexpr int E = M::E, KB = M::KB, STEP = 16 * KB, NK = PP / (4 * E), NP = PP / 16, ROWS = Shape::kRows, STRIDE = kWaves * STEP, SL = Shape::kSlice, LD = Shape::kLd;
+    // What a rounding to bf16 leaves of a probability goes through a second product, and 15 bits of it count (half a step, 2^-8, of a
+    // rest of at most 2^-7).  That costs the matrix unit time that memory leaves over: 64 sequences, one token, 116 us with and
+    // without.  With 32 rows one rounding is all: the second product would take up to 5 % there (heads of 80, two prompts of 512: 97
+    // and 102 us), and 18 to 35 % in the kernel of many rows.  The first part is kept below the whole, so that the rest is above
+    // zero like it: an infinite value then gives the same infinity twice.
+    constexpr bool REST = sizeof(T) == 2 && MB == 1;
     struct Index { TreeLds tree; uint32_t bits[kMaxNodes * kMaxWords]; };
     __shared__ union { Index index; float o[kWaves][ROWS][LD]; int64_t first[kThreads + 1]; } lds;
     __shared__ float ml[kWaves][ROWS][2];
@@ -297,21 +303,24 @@ __global__ __launch_bounds__(kThreads, (StreamShape<T, PP, MB>::kMinWaves)) void
             for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) p[mb][e] = __builtin_amdgcn_exp2f(fmaf(p[mb][e], scale, -base[mb]));
-                const Frag pf = M::round(p[mb]);
-                l[mb] = sum_of(pf, l[mb]);
+                if constexpr (REST) {
+                    float most[E];
 #pragma unroll
-                for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
-                if (MB == 1 && sizeof(T) == 2) {
-                    // What the rounding left, in a second product: 16 bits of a probability.  It costs the matrix unit time that
-                    // memory leaves over (64 sequences, one token: 116 us with and without).  With 32 rows it is one rounding: the
-                    // second product would take up to 5 % there (heads of 80, two prompts of 512: 97 and 102 us), and 18 to 35 % in
-                    // the kernel of many rows.
+                    for (int e = 0; e < E; ++e) most[e] = p[mb][e] * (1.f - 0x1p-8f);
+                    const Frag pf = M::round(most);
 #pragma unroll
                     for (int e = 0; e < E; ++e) p[mb][e] -= (float)pf[e];
                     const Frag rest = M::round(p[mb]);
-                    l[mb] = sum_of(rest, l[mb]);
+                    l[mb] = sum_of(rest, sum_of(pf, l[mb]));
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
 #pragma unroll
                     for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], rest, o[mb][x]);
+                } else {
+                    const Frag pf = M::round(p[mb]);   // bf16: one rounding of each probability, and their sum is the rounded ones'
+                    l[mb] = sum_of(pf, l[mb]);
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) o[mb][x] = M::pv(vf[x], pf, o[mb][x]);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
