@@ -384,7 +384,8 @@ typedef struct stree_kv {
 
 enum stree_attn_flags {
     STREE_ROPE_INTERLEAVED = 1, /* stree_tree_rope: pairs (2j, 2j+1); otherwise (j, j + rotary_dim/2) */
-    STREE_ATTN_PLAIN = 256      /* the plain kernels even where a tuned one applies (same results to rounding) */
+    STREE_ATTN_PLAIN = 256      /* stree_tree_attn: the plain kernel even where a tuned one applies (same results to
+                                   rounding); no other call looks at it */
 };
 
 /* Sizes of one attention layer's pass over the nodes.  POD, host memory. */
@@ -447,9 +448,12 @@ int stree_tree_rope(const stree_attn *a, const stree_kv *kv, const int32_t *pare
  * that may run at the same time need their own.  Sums, maxima and parts are fp32.  The tuned kernels round bf16's
  * probabilities for the matrix units (their sum is that of the rounded ones): to 15 bits where a key/value head has up to
  * 16 rows (nnodes * nheads / nheads_kv), to bf16's 8 where there are more.
- * Infinities and NaN in the keys or values of a node reach the nodes that see it and no others.
- * Tuned kernels: headdim a multiple of 8 (bf16) or 4 (fp32), 16-byte aligned q, k, v, out and a q stride of whole
- * 16-byte pieces; a plain kernel takes the rest.
+ * Infinities and NaN in the keys or values of a node reach the nodes that see it and no others.  Sums are relative to a
+ * maximum that may lag by a factor of 2^8 and are divided at the end: they are finite as long as keys * the largest |V|
+ * stays below 2^120, and a weight below 2^-118 may count with up to that.
+ * Tuned kernels: headdim a multiple of 8 (bf16) or 4 (fp32), 16-byte aligned q, k, v, out, a q stride of whole
+ * 16-byte pieces, fewer than 65536 pairs of a sequence and a key/value head and 2^24 rows to one; a plain kernel, slow
+ * where there is much to do, takes the rest.
  */
 int stree_tree_attn(const stree_attn *a, const stree_kv *kv, const int32_t *parent, const int32_t *lengths,
                     const void *q, void *out, int32_t *seq_status, void *workspace, size_t workspace_bytes,
@@ -495,7 +499,8 @@ int stree_resize_kv(const stree_kv *kv, const stree_pool *pool, int32_t batch, c
 /*
  * Sequences forked: for f < nforks sequence dst[f], which holds no pages, becomes a copy of src[f] (lengths, and as far
  * as its text goes): full pages are shared, the page that src's last tokens stand in, if it is not full, is copied to a
- * free page, whole, in every layer.  So no shared page is ever written to by appending.  The same src may be forked any
+ * free page, whole, in every layer.  So no shared page is ever written to by appending, as long as neither sequence's
+ * text gets shorter than it was at the fork.  The same src may be forked any
  * number of times.  fork_status [nforks] (required) gets 0, or, with nothing done for that fork,
  *   STREE_SEQ_LENGTH  src or dst outside [0, batch), src idle, or its length beyond the pages that it holds
  *   STREE_SEQ_PAGE    a page of src has a bad number or is held by nobody

@@ -9,10 +9,11 @@
 // barrier and no shuffle in the loop: the maximum is moved only when a score passes it by kSlack (2^kSlack is harmless in
 // fp32), which a vote finds out.  Waves are joined through LDS at the end, pieces by a second kernel.
 //
-// Bound by memory: 16 rows take 256 cycles of the matrix unit per 32 keys where the chip's memory needs 5000 to bring them.  Heads
-// of 128 in bf16, 4 rows of 8 key/value heads: 64 sequences of up to 4096 tokens 116 us (671 MB, 5.8 TB/s), one of 131071 100 us
-// (537 MB, 5.4 TB/s); a read of nothing but such pages reaches 6.8 TB/s here.  fp32, 60 rows behind 500 tokens: 16.7 us, of which
-// 3.9 join parts, the rest is the chain launch -> lengths -> pages -> keys -> products.
+// Bound by memory: 16 rows take 384 cycles of the matrix unit per 32 keys (bf16, heads of 128) where the chip's memory needs 5000 to
+// bring them.  4 rows of 8 key/value heads: 64 sequences of up to 4096 tokens 116 us (676 MB, 5.8 TB/s), one of 131071 100 us
+// (537 MB, 5.4 TB/s); a read of nothing but such pages reaches 6.8 TB/s here.  fp32, 64 sequences of up to 2048 124 us (677 MB,
+// 5.5 TB/s); 60 rows behind 500 tokens 16.5 us, of which 3.9 join parts, the rest is the chain launch -> lengths -> pages -> keys
+// -> products.
 #include "attn.hpp"
 
 namespace stree {
@@ -503,7 +504,10 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, KvView<
 // two tiles 300; 16 of 2000, 36 rows: 46 and 50; 32 rows: 46, here 40).  Only one short sequence is better off here (60 rows behind
 // 500 tokens: 19 and 15 us).  Tiles of 64 rows up to 128, of 256 beyond (16 sequences of 2000 tokens, 128 rows in two tiles 62 us, in
 // half of one 70; 192 rows in three 119, in one 69).  Here one tile of 32 rows rather than two of 16: 64 sequences of 4000 tokens
-// 170 us, not 276.
+// 170 us, not 276.  That holds although the kernels of 32 rows and heads of more than 64 spill registers (heads of 128 56 of them in
+// bf16, 72 in fp32, heads of 80 and 96 214 and 114, of 256 166 and 197; with 16 rows at most 8): 16 sequences of 2000 tokens, 64 rows,
+// fp32 heads of 128 117 us, with 16 147; bf16 heads of 80 49 and 68, of 256 116 and 142.  Two shapes go the other way and are not
+// told apart: fp32 heads of 256 (64 rows 320 us, with 16 273; 32 rows 182 and 150) and bf16 heads of 192 (32 rows 83 and 78).
 struct Shape {
     int blocks, tiles, workers;
     bool shared;                                     // the kernel that shares tiles of keys through LDS
@@ -524,7 +528,9 @@ struct Shape {
         crowd(kChip * (kv.headdim <= 128 ? 2 : 1), most);                            // (kMinWaves)
     }
     // As many workers as `chip` workgroups make; on one XCD each where that leaves out an eighth of them at most (a prompt of 8192
-    // tokens, 128 tiles of rows: two workers on two of the eight XCDs took 2436 us, spread out 630).
+    // tokens, 128 tiles of rows: two workers on two of the eight XCDs took 2436 us, spread out 630).  Workers are whole numbers, so
+    // tiles just beyond a half, or the whole, of the chip leave nearly half of it idle: 8256 tokens, 129 tiles, 1140 us; 16448, 257
+    // tiles, 4700.
     void crowd(int chip, int64_t most) {
         int w = chip / tiles < 1 ? 1 : chip / tiles;
         spread = w / 8 * 64 < w * 7;

@@ -8,11 +8,13 @@
 // their way; one barrier a tile.  The first product of the next 32 keys is issued with the exponentials of these, which it does
 // not wait for.
 //
-// With 256 rows a tile takes 2048 cycles of a SIMD's matrix unit, about as many of LDS reads and as many of exponentials and sums.
-// What bounds it is the chip's power: at 64 rows of 131000 tokens (537 MB) the clock falls to 1.6 GHz, and a tile takes 2.25 us;
-// where the keys come from L2 (less to move) 1.6.  Short calls keep 1.9 GHz and spend 10 us on the chain to the first tile and
-// 12 us on parts: 16 trees of 64 nodes behind 2900 tokens on average 89 to 96 us (44.6 Gflop, 190 MB), of which 12 join parts; two
-// prompts of 512 behind 1537 69 to 74 us, of which 12; one of 8192 630 us (550 Gflop, 0.88 Pflop/s).  Tried beside this: 64 rows a
+// With 256 rows a tile takes 2048 cycles of a SIMD's matrix unit, about as many of LDS reads and as many of exponentials and sums,
+// and two waves a SIMD overlap the three in part only: that bounds it, at some 3800 cycles a tile (2 us a CU at the 1.9 GHz that
+// the clock then has).  Around the tiles stand 10 us of the chain to the first one and two ends of a share, so that of the whole
+// kernel's cycles the matrix units are busy in 22 %.  The clock falls further where there is more to move, to 1.6 GHz at 64 rows of
+// 131000 tokens (537 MB): 2.25 us a tile; where the keys come from L2 1.6.  16 trees of 64 nodes behind 2900 tokens on average
+// 89 to 96 us (44.6 Gflop, 190 MB), of which 12.6 join parts; two prompts of 512 behind 1537 69 to 74 us, of which 12; one of 8192
+// 615 to 630 us (550 Gflop, 0.88 Pflop/s), with 64 tokens more 1140 (Shape::crowd).  Tried beside this: 64 rows a
 // wave, half the LDS reads, one wave a SIMD (138 us where this took 99: accumulators move between two register files), 128 rows and
 // two workgroups a CU (108 and 97), the streaming hint (the prompts: 88 and 80, tiles of rows share keys in L2).
 #include "attn.hpp"

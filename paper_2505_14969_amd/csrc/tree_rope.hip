@@ -1,8 +1,10 @@
 // stree_tree_rope: per head of q and k an RMS norm and the rotation to the node's position, k and v appended to the paged cache.
 //   x^ = x / sqrt(mean x^2 + eps) * w;  pairs (u, w) turn by 2 pi frac(position * turns[j]), frac in 64 bits
-// Rows are read once and written once: bound by memory where there are many, two fp32 prompts of 2047 tokens with 32 + 8 + 8 heads of
-// 128 40 us (201 MB, 5.0 TB/s); else by the chain length -> tree, pages -> angles -> rows: one token 5.7 us, 16 trees of 64 nodes
-// 13.3 us (25 MB, 6 us at that rate); the angles, which every group of heads works out for itself, are 0.6 of them.
+// Rows are read once and written once: bound by memory where there are many in fp32, two prompts of 2047 tokens with 32 + 8 + 8 heads
+// of 128 40 us (201 MB, 5.0 TB/s); in bf16, with twice the values a byte, by the workgroups of q and k and not by memory: four of 2048
+// 54 us (201 MB, 3.7 TB/s; without the workgroups of v, which read their rows twice, 51), one of 65536 370 us (4.4 TB/s).  Few nodes are
+// bound by the chain length -> tree, pages -> angles -> rows: one token 5.4 us, 16 trees of 64 nodes 12.7 to 14 us (25 MB, 6 us at
+// the fp32 rate); the angles, which every group of heads works out for itself, are 0.6 of them.
 #include "kv.hpp"
 #include "launch_kv.hpp"
 
