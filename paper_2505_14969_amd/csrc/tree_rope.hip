@@ -3,7 +3,7 @@
 // Rows are read once and written once: bound by memory where there are many in fp32, two prompts of 2047 tokens with 32 + 8 + 8 heads
 // of 128 40 us (201 MB, 5.0 TB/s); in bf16, with twice the values a byte, by the workgroups of q and k and not by memory: four of 2048
 // 54 us (201 MB, 3.7 TB/s; without the workgroups of v, which read their rows twice, 51), one of 65536 370 us (4.4 TB/s).  Few nodes are
-// bound by the chain length -> tree, pages -> angles -> rows: one token 5.4 us, 16 trees of 64 nodes 12.7 to 14 us (25 MB, 6 us at
+// bound by the chain length -> tree, pages -> angles -> rows: one token 5.4 us, 16 trees of 64 nodes 12.7 to 14.6 us (25 MB, 6 us at
 // the fp32 rate); the angles, which every group of heads works out for itself, are 0.6 of them.
 #include "kv.hpp"
 #include "launch_kv.hpp"
@@ -150,9 +150,10 @@ struct Piece<float> {
 // to HC heads of q, of k or of v).  q and k: TL lanes hold a row, 16 bytes each; a team stays with its node, whose cosines and
 // sines it keeps, and all of its rows are requested at once.  Pairs half the rotated columns apart are another lane's 16 bytes.
 // v: turned round in LDS, so that 16 bytes of a column of the tile go out at once.
-// Every workgroup looks at the page numbers of all nodes' slots before it writes; of a long prompt it then takes a tile after the
-// other, every gridDim.x-th (node_groups()).
-template <typename T, int TL, int HC, bool HALF>
+// Every workgroup looks at the page numbers of all nodes' slots before it writes; of a long prompt (LONG) it then takes a tile after
+// the other, every gridDim.x-th (node_groups()).  Others leave behind their one tile, which takes fewer registers: 80 and not 97 for
+// four bf16 heads of 128, six waves a SIMD and not four (63 trees of 4 nodes 12.0 us and not 14.1).
+template <typename T, int TL, int HC, bool HALF, bool LONG>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv, int zq, int zk) {
     constexpr int E = Piece<T>::E, TEAMS = kThreads / TL;
     __shared__ TreeLds tree;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
                 }
                 __syncthreads();
             }
-            if (a.n - node0 <= stride) return;
+            if (!LONG || a.n - node0 <= stride) return;
             slot0 += stride, node0 += stride;
             pg = kv.page_of(b, slot0);
         }
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
                 if (node0 + s >= 0 && node0 + s < a.n && c < pieces)
                     for (int h = 0; h < heads; ++h)
                         *reinterpret_cast<uint4 *>(out + ((row0 + node0 + s) * a.heads + h0 + h) * P + c * E) = make_uint4(0u, 0u, 0u, 0u);
-            if (a.n - node0 <= stride) return;
+            if (!LONG || a.n - node0 <= stride) return;
         }
     }
     const int half = a.rotary / 2;
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
             }
             if (s0 + TEAMS < kSlots) request(s + TEAMS);
         }
-        if (a.n - node0 <= stride) return;
+        if (!LONG || a.n - node0 <= stride) return;
         slot0 += stride, node0 += stride;
         pg = kv.page_of(b, slot0);
         request(tid / TL);
@@ -325,8 +326,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, KvView<T> kv
 // there are more page numbers, all of which every workgroup looks at, than a workgroup has threads.  Then as many in all as the chip
 // holds at once, so that the time grows with a prompt and not with its square (131072 tokens of 8 + 2 + 2 heads of 128 205 us,
 // with a workgroup a tile 297; a million of one head of 16 0.41 ms and 4.6).
+constexpr int kLong = 16 * kThreads;   // nodes, in pages of 16
 inline unsigned node_groups(int n, int64_t steps, int64_t others) {
-    if (n <= 16 * kThreads) return (unsigned)steps;
+    if (n <= kLong) return (unsigned)steps;
     const int64_t most = others < 2048 ? 2048 / others : 1;
     return (unsigned)(steps < most ? steps : most);
 }
@@ -334,10 +336,19 @@ inline unsigned node_groups(int n, int64_t steps, int64_t others) {
 template <typename T, int TL, int HC>
 void launch_tuned(const RopeArgs &a, const stree_kv &kv, int batch, hipStream_t st) {
     const int zq = (a.heads + HC - 1) / HC, zk = (kv.nheads_kv + HC - 1) / HC;
-    const int z = zq + 2 * zk;
-    const dim3 grid(node_groups(a.n, (a.n + 2 * kSlots - 2) / kSlots, (int64_t)batch * z), (unsigned)batch, (unsigned)z);
-    if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, TL, HC, false>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
-    else hipLaunchKernelGGL((rope_kernel<T, TL, HC, true>), grid, dim3(kThreads), 0, st, a, KvView<T>(kv), zq, zk);
+    const int tiles = (a.n + 2 * kSlots - 2) / kSlots;
+    dim3 grid((unsigned)tiles, (unsigned)batch, (unsigned)(zq + 2 * zk));
+    const KvView<T> view(kv);
+    if constexpr (HC > 2) {                            // (two heads a workgroup are for few nodes)
+        if (a.n > kLong) {
+            grid.x = node_groups(a.n, tiles, (int64_t)batch * grid.z);
+            if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, TL, HC, false, true>), grid, dim3(kThreads), 0, st, a, view, zq, zk);
+            else hipLaunchKernelGGL((rope_kernel<T, TL, HC, true, true>), grid, dim3(kThreads), 0, st, a, view, zq, zk);
+            return;
+        }
+    }
+    if (a.interleaved) hipLaunchKernelGGL((rope_kernel<T, TL, HC, false, false>), grid, dim3(kThreads), 0, st, a, view, zq, zk);
+    else hipLaunchKernelGGL((rope_kernel<T, TL, HC, true, false>), grid, dim3(kThreads), 0, st, a, view, zq, zk);
 }
 
 template <typename T>
